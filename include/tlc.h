@@ -56,6 +56,7 @@ extern "C" {
 #define TLC_E_NONFINITE (-3) /* NaN/Inf in tensor+residual, or max*s overflows */
 #define TLC_E_CORRUPT (-4)   /* compressed stream does not expand to ceil(n/5) bytes */
 #define TLC_E_DEVICE (-5)    /* HIP runtime error, or the context is unusable */
+#define TLC_E_INDEX (-6)     /* a token id outside the embedding table */
 
 /* Largest number of values one call accepts, summed over a batch (the
  * quartic byte counts must fit the 30-bit counters of the zero-run scans). */
@@ -254,6 +255,121 @@ int tlc_compress_noalloc(const float* tensor, float* residual, size_t n, float s
                          uint8_t* bytes, size_t bytes_cap, tlc_result* result,
                          void* hip_stream);
 
+/* ---- before the codec: embedding tables, gradient norm and clipping ------
+ *
+ * What a training step of a language model runs around tlc_compress: the
+ * lookup of its tokens' embedding rows, the gradient of the embedding table
+ * (fp32, dense, rows without a token exactly zero: a tensor that zero-run
+ * encoding shortens well), and the clipping of all gradients by their global
+ * norm, written as the fp32 tensors that tlc_compress reads.
+ *
+ * They run on a context of their own, bound to one HIP stream like a tlc_ctx:
+ * asynchronous on that stream, no device memory allocated per call, tensors
+ * device memory owned by the caller, the same rules for host threads and
+ * errors.  The calls with ids may be captured into a graph; those over lists
+ * of tensors hand their descriptors over in host memory that later calls use
+ * again, and may not. */
+typedef struct tlc_train tlc_train;
+
+/* Types of values and of token ids. */
+#define TLC_F32 0
+#define TLC_BF16 1
+#define TLC_F16 2
+#define TLC_I32 0
+#define TLC_I64 1
+
+/* Largest table height and row length. */
+#define TLC_MAX_ROWS 2147483646
+#define TLC_MAX_DIM 16777216
+
+/* Create a context on `hip_stream` for embedding gradients of up to
+ * max_tokens tokens (below 2^31) into tables of up to max_rows rows of up to
+ * max_dim values, and for lists of up to max_tensors tensors (at most
+ * TLC_MAX_TENSORS).  Any of them may be 0: that call is then refused
+ * (tlc_embedding needs none of them). */
+int tlc_train_create(tlc_train** ctx, size_t max_tokens, size_t max_rows, size_t max_dim,
+                     size_t max_tensors, void* hip_stream);
+
+/* Wait for the context's outstanding work and free it.  NULL is a no-op. */
+int tlc_train_destroy(tlc_train* ctx);
+
+/* Wait for all work of the context and return (then clear) the sticky
+ * status of its lookups and embedding gradients: TLC_OK or TLC_E_INDEX. */
+int tlc_train_sync(tlc_train* ctx);
+
+/* Embedding lookup with scaling: for every token t
+ *   out[t, k] = round(scale * table[ids[t], k]),  0 <= k < dim,
+ * the product in fp32, rounded once (half to even) to out's type.
+ *   table       device, `rows` rows of dim values of table_type, the first
+ *               values of two rows table_stride values apart (any stride).
+ *   ids         device int32 or int64 [count] (ids_type).
+ *   out         device, count rows of dim values of out_type, out_stride >=
+ *               dim values apart; must not overlap table or ids.
+ *   scale       finite.
+ * An id outside [0, rows) gives a row of zeros, and the next
+ * tlc_train_sync() returns TLC_E_INDEX. */
+int tlc_embedding(tlc_train* ctx, const void* table, int table_type, size_t rows, size_t dim,
+                  size_t table_stride, const void* ids, int ids_type, size_t count, float scale,
+                  void* out, int out_type, size_t out_stride);
+
+/* The gradient of an embedding table: for every row v
+ *   out[v, k] = (accumulate ? out[v, k] : 0) + scale * sum grad[t, k]
+ * over the tokens t with ids[t] == v.  fp32 sums; the order in which they
+ * are formed is fixed by the sizes, types and ids, so that the same call gives the
+ * same bits.  A row without a token becomes 0, or with accumulate stays as it
+ * is, bit for bit.
+ *   grad        device, count rows of dim values of grad_type, grad_stride
+ *               values apart (0: one row for all tokens).
+ *   padding_id  tokens with this id add nothing (negative: there are none).
+ *   out         device fp32, `rows` rows of dim values out_stride >= dim
+ *               values apart; values between rows are left alone.  Must not
+ *               overlap grad or ids.
+ * An id outside [0, rows) adds nothing, and the next tlc_train_sync()
+ * returns TLC_E_INDEX.  The rows of grad of tokens that add nothing are not
+ * part of any sum, whatever they hold. */
+int tlc_embedding_grad(tlc_train* ctx, const void* grad, int grad_type, size_t grad_stride,
+                       const void* ids, int ids_type, size_t count, size_t rows, size_t dim,
+                       float scale, int64_t padding_id, float* out, size_t out_stride,
+                       int accumulate);
+
+/* Result of the calls on lists of tensors, in device memory. */
+typedef struct tlc_norm_result {
+  double sumsq;      /* sum of the squares of all values, in 64 bits */
+  float norm;        /* sqrt(sumsq), rounded to fp32 */
+  float coef;        /* the factor of the values: 1 where norm <= max_norm, else max_norm / norm */
+  int32_t status;    /* TLC_OK, or TLC_E_NONFINITE: NaN/Inf among the values (coef is NaN) */
+  uint32_t reserved; /* 0 */
+} tlc_norm_result;
+
+/* The global norm of `count` tensors: result->sumsq, norm and status (coef is
+ * 1).  Host arrays of device pointers, of types and of value counts (each at
+ * most TLC_MAX_N, 2^40 in all); a tensor of no values may be NULL.  Squares and sums are
+ * in 64 bits: no value of any type overflows them, and the order of the sums,
+ * fixed by the sizes, is not seen in the norm. */
+int tlc_grad_norm(tlc_train* ctx, size_t count, const void* const* tensors, const int* types,
+                  const size_t* ns, tlc_norm_result* result);
+
+/* Clip `count` tensors by a norm that is known: with norm =
+ * sqrt(result->sumsq) and coef = norm > max_norm ? max_norm / norm : 1 (64
+ * bits, rounded to fp32),
+ *   outs[i][k] = coef * tensors[i][k]   (one fp32 product)
+ * for every tensor; also writes result's norm, coef and status.  A program
+ * whose gradients are spread over ranks adds up the sumsq of tlc_grad_norm
+ * (of its shards) between the two calls.
+ *   max_norm    finite, >= 0.
+ *   outs        fp32 buffers; outs[i] may be tensors[i] itself where that is
+ *               fp32.  NULL: in place in the tensors' own types (rounded half
+ *               to even; with coef 1 nothing is written).
+ * No buffer may overlap another one that is written.  If sumsq is not finite
+ * no buffer is written. */
+int tlc_clip(tlc_train* ctx, size_t count, const void* const* tensors, const int* types,
+             const size_t* ns, float max_norm, tlc_norm_result* result, float* const* outs);
+
+/* tlc_grad_norm followed by tlc_clip. */
+int tlc_clip_grad_norm(tlc_train* ctx, size_t count, const void* const* tensors,
+                       const int* types, const size_t* ns, float max_norm,
+                       tlc_norm_result* result, float* const* outs);
+
 /* ---- options ------------------------------------------------------------ */
 
 /* TLC_OPT_IN_PLACE_FEEDBACK: take step 1 of error accumulation (Section
@@ -324,7 +440,7 @@ const char* tlc_last_error_string(void);
 #define TLC_KERNEL_COUNT 18
 
 /* Enable (on != 0) or disable recording of a start/stop event pair around
- * every kernel launch of the context (of the kernels selected by
+ * every kernel launch of the tlc_ctx (of the kernels selected by
  * tlc_profile_mask; all of them by default). */
 int tlc_profile_enable(tlc_ctx* ctx, int on);
 

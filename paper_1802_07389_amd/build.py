@@ -11,8 +11,10 @@ LIB = os.path.join(PKG, "libtlc.so")
 # a pseudo-random while first (TLC_DELAY_INJECT); used only by
 # tests/test_gpu_lookback_delays.py.
 LIB_DELAY = os.path.join(PKG, "libtlc_delay.so")
-SOURCES = ["encode.hip", "decode.hip", "int8.hip", "tlc_api.hip", "noalloc.hip"]
-HEADERS = ["tlc_internal.h", "device_common.hpp", "lookback.hpp", "wave_scan.hpp", "zre_scan.hpp"]
+SOURCES = ["encode.hip", "decode.hip", "int8.hip", "tlc_api.hip", "noalloc.hip",
+           "embedding.hip", "norm.hip", "train_api.hip"]
+HEADERS = ["tlc_internal.h", "device_common.hpp", "lookback.hpp", "wave_scan.hpp", "zre_scan.hpp",
+           "api_common.hpp", "train_internal.h", "typed_io.hpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

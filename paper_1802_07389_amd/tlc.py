@@ -22,6 +22,7 @@ TLC_E_CAPACITY = -2
 TLC_E_NONFINITE = -3
 TLC_E_CORRUPT = -4
 TLC_E_DEVICE = -5
+TLC_E_INDEX = -6
 
 TLC_MAX_N = 4294967295
 TLC_MAX_TENSORS = 65536
@@ -57,6 +58,14 @@ TLC_MODE_NO_ZRE = 1
 TLC_MODE_STOCHASTIC = 2
 TLC_MODE_INT8 = 3
 
+TLC_F32 = 0
+TLC_BF16 = 1
+TLC_F16 = 2
+TLC_I32 = 0
+TLC_I64 = 1
+TLC_MAX_ROWS = 2147483646
+TLC_MAX_DIM = 16777216
+
 EXPORTS = (
     "tlc_max_compressed_bytes", "tlc_ctx_create", "tlc_ctx_create_batch",
     "tlc_ctx_destroy", "tlc_compress", "tlc_compress_ex", "tlc_compress_batch",
@@ -65,6 +74,8 @@ EXPORTS = (
     "tlc_last_error_string", "tlc_profile_enable", "tlc_profile_mask", "tlc_profile_get",
     "tlc_profile_reset", "tlc_kernel_name", "tlc_ctx_set_options",
     "tlc_compress_noalloc", "tlc_ctx_set_epochs",
+    "tlc_train_create", "tlc_train_destroy", "tlc_train_sync", "tlc_embedding",
+    "tlc_embedding_grad", "tlc_grad_norm", "tlc_clip", "tlc_clip_grad_norm",
 )
 
 
@@ -73,6 +84,13 @@ class tlc_result(ctypes.Structure):
     tlc_compress_noalloc; this layout reads a host copy of it)."""
     _fields_ = [("status", ctypes.c_int32), ("bytes_len", ctypes.c_uint32),
                 ("scale", ctypes.c_float), ("reserved", ctypes.c_uint32)]
+
+
+class tlc_norm_result(ctypes.Structure):
+    """struct tlc_norm_result of tlc.h (device memory; this layout reads a
+    host copy of it)."""
+    _fields_ = [("sumsq", ctypes.c_double), ("norm", ctypes.c_float), ("coef", ctypes.c_float),
+                ("status", ctypes.c_int32), ("reserved", ctypes.c_uint32)]
 
 
 class TLCError(RuntimeError):
@@ -135,6 +153,23 @@ def _load():
     L.tlc_compress_noalloc.restype = i
     L.tlc_ctx_set_epochs.argtypes = [vp, ctypes.c_uint32, ctypes.c_uint32]
     L.tlc_ctx_set_epochs.restype = i
+    L.tlc_train_create.argtypes = [P(vp), sz, sz, sz, sz, vp]
+    L.tlc_train_create.restype = i
+    L.tlc_train_destroy.argtypes = [vp]
+    L.tlc_train_destroy.restype = i
+    L.tlc_train_sync.argtypes = [vp]
+    L.tlc_train_sync.restype = i
+    L.tlc_embedding.argtypes = [vp, vp, i, sz, sz, sz, vp, i, sz, f, vp, i, sz]
+    L.tlc_embedding.restype = i
+    L.tlc_embedding_grad.argtypes = [vp, vp, i, sz, vp, i, sz, sz, sz, f, ctypes.c_int64, vp, sz,
+                                     i]
+    L.tlc_embedding_grad.restype = i
+    L.tlc_grad_norm.argtypes = [vp, sz, P(vp), P(i), P(sz), vp]
+    L.tlc_grad_norm.restype = i
+    L.tlc_clip.argtypes = [vp, sz, P(vp), P(i), P(sz), f, vp, P(vp)]
+    L.tlc_clip.restype = i
+    L.tlc_clip_grad_norm.argtypes = [vp, sz, P(vp), P(i), P(sz), f, vp, P(vp)]
+    L.tlc_clip_grad_norm.restype = i
     return L
 
 
@@ -248,6 +283,56 @@ def tlc_compress_noalloc(tensor, residual, n, s, bytes_, bytes_cap, result, hip_
 
 def tlc_ctx_set_epochs(ctx, enc_epoch, dec_epoch):
     return lib.tlc_ctx_set_epochs(ctx, int(enc_epoch), int(dec_epoch))
+
+
+def tlc_train_create(max_tokens, max_rows, max_dim, max_tensors, hip_stream):
+    """Return the handle (int) of a training-step context."""
+    h = ctypes.c_void_p()
+    _check(lib.tlc_train_create(ctypes.byref(h), max_tokens, max_rows, max_dim, max_tensors,
+                                hip_stream))
+    return h.value
+
+
+def tlc_train_destroy(ctx):
+    return lib.tlc_train_destroy(ctx)
+
+
+def tlc_train_sync(ctx):
+    return lib.tlc_train_sync(ctx)
+
+
+def tlc_embedding(ctx, table, table_type, rows, dim, table_stride, ids, ids_type, count, scale,
+                  out, out_type, out_stride):
+    return lib.tlc_embedding(ctx, table, table_type, rows, dim, table_stride, ids, ids_type,
+                             count, scale, out, out_type, out_stride)
+
+
+def tlc_embedding_grad(ctx, grad, grad_type, grad_stride, ids, ids_type, count, rows, dim, scale,
+                       padding_id, out, out_stride, accumulate):
+    return lib.tlc_embedding_grad(ctx, grad, grad_type, grad_stride, ids, ids_type, count, rows,
+                                  dim, scale, padding_id, out, out_stride, int(bool(accumulate)))
+
+
+def _list_args(tensors, types, ns):
+    return (_arr(ctypes.c_void_p, tensors), _arr(ctypes.c_int, types), _arr(ctypes.c_size_t, ns))
+
+
+def tlc_grad_norm(ctx, tensors, types, ns, result):
+    """Lists of device pointers, types and value counts; result: device
+    address of a tlc_norm_result."""
+    return lib.tlc_grad_norm(ctx, len(tensors), *_list_args(tensors, types, ns), result)
+
+
+def tlc_clip(ctx, tensors, types, ns, max_norm, result, outs=None):
+    """outs: a list of device pointers, or None: in place."""
+    return lib.tlc_clip(ctx, len(tensors), *_list_args(tensors, types, ns), max_norm, result,
+                        None if outs is None else _arr(ctypes.c_void_p, outs))
+
+
+def tlc_clip_grad_norm(ctx, tensors, types, ns, max_norm, result, outs=None):
+    """outs: a list of device pointers, or None: in place."""
+    return lib.tlc_clip_grad_norm(ctx, len(tensors), *_list_args(tensors, types, ns), max_norm,
+                                  result, None if outs is None else _arr(ctypes.c_void_p, outs))
 
 
 def tlc_profile_enable(ctx, on):
@@ -417,3 +502,172 @@ class Context:
         st, ms, cnt = tlc_profile_get(self.handle, kernel)
         _check(st)
         return ms, cnt
+
+
+# ----------------------------------------------------------------- training step
+_TYPES = {torch.float32: TLC_F32, torch.bfloat16: TLC_BF16, torch.float16: TLC_F16}
+_ID_TYPES = {torch.int32: TLC_I32, torch.int64: TLC_I64}
+
+
+def _type_of(t, name):
+    code = _TYPES.get(t.dtype)
+    if code is None or not t.is_cuda:
+        raise ValueError(f"{name} must be a float32, bfloat16 or float16 GPU tensor")
+    return code
+
+
+def _matrix(t, name):
+    """(pointer, type, row stride) of a tensor of rows: two dimensions with
+    neighbouring values in a row, or more and contiguous."""
+    code = _type_of(t, name)
+    if t.dim() == 2:
+        stride, step = t.stride()
+        if step != 1 and t.shape[1] > 1:
+            raise ValueError(f"{name} must have its rows' values next to each other")
+        return t.data_ptr(), code, stride if t.shape[0] > 1 else t.shape[1]
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous, or a matrix")
+    return t.data_ptr(), code, t.shape[-1]
+
+
+def _token_ids(t):
+    code = _ID_TYPES.get(t.dtype)
+    if code is None or not t.is_cuda or not t.is_contiguous():
+        raise ValueError("ids must be a contiguous int32 or int64 GPU tensor")
+    return t.data_ptr(), code
+
+
+class TensorList:
+    """Tensors of one list call with their arguments laid out once: a program
+    whose gradients keep their buffers makes it once.  It keeps the tensors
+    alive, and follows their values, not a tensor that takes their place."""
+
+    def __init__(self, tensors, outs=None):
+        self.tensors = list(tensors)
+        self.outs = None if outs is None else list(outs)
+        for t in self.tensors:
+            if not t.is_contiguous():
+                raise ValueError("every tensor of a list must be contiguous")
+        self.count = len(self.tensors)
+        if self.outs is not None:
+            if [o.numel() for o in self.outs] != [t.numel() for t in self.tensors]:
+                raise ValueError("tensors and outs differ in their sizes")
+            self.out_ptrs = _arr(ctypes.c_void_p, [_dev_f32(o, "out") for o in self.outs])
+        else:
+            self.out_ptrs = None
+        self.args = _list_args([t.data_ptr() for t in self.tensors],
+                               [_type_of(t, "tensor") for t in self.tensors],
+                               [t.numel() for t in self.tensors])
+
+
+class NormResult:
+    """A tlc_norm_result in device memory, and 0-dim views of its fields."""
+
+    def __init__(self, device):
+        self.buffer = torch.zeros(3, dtype=torch.float64, device=device)
+        self.ptr = self.buffer.data_ptr()
+        words = self.buffer.view(torch.float32)
+        self.sumsq, self.norm, self.coef = self.buffer[0], words[2], words[3]
+        self.status = self.buffer.view(torch.int32)[4]
+
+
+class TrainContext:
+    """The training-step operators around the codec, on one stream: embedding
+    lookups and gradients, the gradient norm and clipping.  Work is ordered on
+    that stream (by default torch's current one when the context is made):
+    tensors that another stream makes or uses are waited for by the caller."""
+
+    def __init__(self, max_tokens=0, max_rows=0, max_dim=0, max_tensors=0, stream=None,
+                 device=None):
+        self.device = torch.device(device) if device is not None else torch.device(
+            "cuda", torch.cuda.current_device())
+        with torch.cuda.device(self.device):
+            self.stream = stream if stream is not None else torch.cuda.current_stream()
+            self.handle = tlc_train_create(int(max_tokens), int(max_rows), int(max_dim),
+                                           int(max_tensors), self.stream.cuda_stream)
+
+    def close(self):
+        if getattr(self, "handle", None):
+            tlc_train_destroy(self.handle)
+            self.handle = None
+
+    __del__ = close
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def embedding(self, table, ids, scale=1.0, out=None, dtype=None):
+        """scale * table[ids] in out's type (a new tensor of `dtype`, by
+        default the table's, where out is None)."""
+        if table.dim() != 2:
+            raise ValueError("table must be a matrix")
+        rows, dim = table.shape
+        if out is None:
+            with torch.cuda.stream(self.stream):
+                out = torch.empty(*ids.shape, dim, dtype=dtype or table.dtype,
+                                  device=self.device)
+        elif out.numel() != ids.numel() * dim or out.shape[-1] != dim:
+            raise ValueError("out has the wrong size")
+        ptr, code, stride = _matrix(table, "table")
+        ids_ptr, ids_code = _token_ids(ids)
+        out_ptr, out_code, out_stride = _matrix(out, "out")
+        _check(lib.tlc_embedding(self.handle, ptr, code, rows, dim, stride, ids_ptr, ids_code,
+                                 ids.numel(), scale, out_ptr, out_code, out_stride))
+        return out
+
+    def embedding_grad(self, grad, ids, out, scale=1.0, padding_id=-1, accumulate=False):
+        """Gradient of embedding()'s table into the float32 matrix out (set, or
+        with accumulate added to)."""
+        if out.dim() != 2 or out.dtype != torch.float32:
+            raise ValueError("out must be a float32 matrix")
+        rows, dim = out.shape
+        if grad.numel() != ids.numel() * dim or grad.shape[-1] != dim:
+            raise ValueError("grad has the wrong size")
+        ptr, code, stride = _matrix(grad, "grad")
+        ids_ptr, ids_code = _token_ids(ids)
+        out_ptr, _, out_stride = _matrix(out, "out")
+        _check(lib.tlc_embedding_grad(self.handle, ptr, code, stride, ids_ptr, ids_code,
+                                      ids.numel(), rows, dim, scale, padding_id, out_ptr,
+                                      out_stride, bool(accumulate)))
+        return out
+
+    def tensor_list(self, tensors, outs=None):
+        """The list of a norm or clipping call, laid out once (outs: float32
+        tensors for the clipped values; None: in place)."""
+        return TensorList(tensors, outs)
+
+    def norm_result(self):
+        """A result buffer to pass to the calls below."""
+        with torch.cuda.stream(self.stream):
+            return NormResult(self.device)
+
+    def grad_norm(self, tensors, result=None):
+        """The global norm of a list of tensors (asynchronous)."""
+        ls = tensors if isinstance(tensors, TensorList) else TensorList(tensors)
+        r = self.norm_result() if result is None else result
+        _check(lib.tlc_grad_norm(self.handle, ls.count, *ls.args, r.ptr))
+        return r
+
+    def clip(self, tensors, max_norm, result, outs=None):
+        """Clip a list by result.sumsq, which grad_norm (and a sum over ranks)
+        left there."""
+        ls = tensors if isinstance(tensors, TensorList) else TensorList(tensors, outs)
+        _check(lib.tlc_clip(self.handle, ls.count, *ls.args, max_norm, result.ptr, ls.out_ptrs))
+        return result
+
+    def clip_grad_norm(self, tensors, max_norm, outs=None, result=None):
+        """Clip a list by its global norm (asynchronous): into outs, or in
+        place.  The result's status is TLC_E_NONFINITE, and nothing written,
+        where a value is NaN or Inf."""
+        ls = tensors if isinstance(tensors, TensorList) else TensorList(tensors, outs)
+        r = self.norm_result() if result is None else result
+        _check(lib.tlc_clip_grad_norm(self.handle, ls.count, *ls.args, max_norm, r.ptr,
+                                      ls.out_ptrs))
+        return r
+
+    def sync(self):
+        """Wait; raises TLCError(TLC_E_INDEX) after an id outside its table."""
+        _check(tlc_train_sync(self.handle))
