@@ -16,16 +16,39 @@ __device__ __forceinline__ int64_t token_row(const void* ids, uint32_t t, uint32
 
 }  // namespace
 
-// One block per token.
-template <class In, class Id, class Out>
-__global__ __launch_bounds__(kEmbThreads) void tlc_embedding_kernel(EmbArgs a) {
-  for (uint32_t t = blockIdx.x; t < a.count; t += gridDim.x) {
-    const int64_t row = token_row<Id>(a.ids, t, a.rows);
-    if (row < 0 && threadIdx.x == 0) host_put(a.bad, 1u);
-    const In* x = static_cast<const In*>(a.x) + (row < 0 ? 0 : row) * a.x_stride;
-    Out* out = static_cast<Out*>(a.out) + t * a.out_stride;
-    for (uint32_t k = threadIdx.x; k < a.dim; k += kEmbThreads)
-      out[k] = row < 0 ? (Out)0.0f : round_to<Out>(a.scale * (float)x[k]);
+// One pass over the output in packs of V values, kUnits of a thread 256 packs
+// apart: the ids of all of them are asked for first, then their rows, then
+// the products stored.  A row that is no whole number of packs ends with a pack
+// moved back to end with it (its values are written twice, alike).
+template <class In, class Id, class Out, int V, int kUnits>
+__global__ __launch_bounds__(kEmbThreads) void tlc_embedding_kernel(EmbArgs a, Divider packs,
+                                                                    uint32_t slice) {
+  const uint32_t t0 = blockIdx.y * slice;
+  const uint32_t units = umin32(slice, a.count - t0) * packs.d;  // below 2^31
+  const uint32_t u0 = blockIdx.x * (kEmbThreads * kUnits) + threadIdx.x;
+  uint32_t t[kUnits], k[kUnits];
+  int64_t row[kUnits];
+#pragma unroll
+  for (int i = 0; i < kUnits; ++i) {
+    const uint32_t u = u0 + i * kEmbThreads;
+    t[i] = quotient(umin32(u, units - 1), packs);
+    k[i] = umin32((umin32(u, units - 1) - t[i] * packs.d) * V, a.dim - V);
+    t[i] += t0;
+    row[i] = token_row<Id>(a.ids, t[i], a.rows);
+  }
+  Pack<In, V> x[kUnits];
+#pragma unroll
+  for (int i = 0; i < kUnits; ++i)
+    x[i] = load_pack<In, V>(static_cast<const In*>(a.x) + (row[i] < 0 ? 0 : row[i]) * a.x_stride +
+                            k[i]);
+#pragma unroll
+  for (int i = 0; i < kUnits; ++i) {
+    if (u0 + i * kEmbThreads >= units) break;
+    Pack<Out, V> o;
+#pragma unroll
+    for (int e = 0; e < V; ++e) o.set(e, row[i] < 0 ? 0.0f : a.scale * x[i].get(e));
+    store_pack<Out, V>(static_cast<Out*>(a.out) + t[i] * a.out_stride + k[i], o);
+    if (row[i] < 0 && k[i] == 0) host_put(a.bad, 1u);
   }
 }
 
@@ -75,30 +98,46 @@ __global__ __launch_bounds__(kEmbThreads) void tlc_embedding_grad_kernel(EmbArgs
 
 namespace {
 
-template <class In, class Id>
-hipError_t embedding_out(const EmbArgs& a, int out_type, uint32_t grid, hipStream_t st) {
-  switch (out_type) {
-    case TLC_F32:
-      launch_k(tlc_embedding_kernel<In, Id, float>, grid, kEmbThreads, st, a);
-      break;
-    case TLC_BF16:
-      launch_k(tlc_embedding_kernel<In, Id, bf16_t>, grid, kEmbThreads, st, a);
-      break;
-    default:
-      launch_k(tlc_embedding_kernel<In, Id, f16_t>, grid, kEmbThreads, st, a);
+template <class In, class Id, class Out, int V>
+hipError_t embedding_packs(const EmbArgs& a, hipStream_t st) {
+  const uint32_t packs = (a.dim + V - 1) / V;
+  const uint32_t slice = std::min(a.count, (uint32_t)((1u << 31) - 1) / packs);
+  const uint32_t slices = (a.count + slice - 1) / slice;
+  const uint32_t units = slice * packs;
+  constexpr int kUnits = 4;
+  // A call that four packs a thread leave without a block for every CU takes
+  // one each.
+  if ((units + kEmbThreads * kUnits - 1) / (kEmbThreads * kUnits) < kCus) {
+    launch_k(tlc_embedding_kernel<In, Id, Out, V, 1>,
+             dim3((units + kEmbThreads - 1) / kEmbThreads, slices), kEmbThreads, st, a,
+             divider(packs), slice);
+  } else {
+    launch_k(tlc_embedding_kernel<In, Id, Out, V, kUnits>,
+             dim3((units + kEmbThreads * kUnits - 1) / (kEmbThreads * kUnits), slices),
+             kEmbThreads, st, a, divider(packs), slice);
   }
   return hipGetLastError();
+}
+
+// 16 bytes of the narrower side a pack; rows shorter than that, value by value.
+template <class In, class Id, class Out>
+hipError_t embedding_rows(const EmbArgs& a, hipStream_t st) {
+  constexpr int V = sizeof(In) == 4 && sizeof(Out) == 4 ? 4 : 8;
+  return a.dim >= V ? embedding_packs<In, Id, Out, V>(a, st)
+                    : embedding_packs<In, Id, Out, 1>(a, st);
 }
 
 }  // namespace
 
 hipError_t launch_embedding(const EmbArgs& a, int table_type, int ids_type, int out_type,
                             hipStream_t st) {
-  const uint32_t grid = std::min(a.count, 1u << 20);
   return with_type(table_type, [&](auto in) {
-    using In = decltype(in);
-    return ids_type == TLC_I64 ? embedding_out<In, int64_t>(a, out_type, grid, st)
-                               : embedding_out<In, int32_t>(a, out_type, grid, st);
+    return with_type(out_type, [&](auto out) {
+      using In = decltype(in);
+      using Out = decltype(out);
+      return ids_type == TLC_I64 ? embedding_rows<In, int64_t, Out>(a, st)
+                                 : embedding_rows<In, int32_t, Out>(a, st);
+    });
   });
 }
 
