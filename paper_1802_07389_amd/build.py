@@ -12,7 +12,7 @@ LIB = os.path.join(PKG, "libtlc.so")
 # tests/test_gpu_lookback_delays.py.
 LIB_DELAY = os.path.join(PKG, "libtlc_delay.so")
 SOURCES = ["encode.hip", "decode.hip", "int8.hip", "tlc_api.hip", "noalloc.hip",
-           "embedding.hip", "norm.hip", "train_api.hip"]
+           "embedding.hip", "embedding_grad.hip", "norm.hip", "train_api.hip"]
 HEADERS = ["tlc_internal.h", "device_common.hpp", "lookback.hpp", "wave_scan.hpp", "zre_scan.hpp",
            "api_common.hpp", "train_internal.h", "typed_io.hpp"]
 

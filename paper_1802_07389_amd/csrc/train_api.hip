@@ -40,6 +40,7 @@ struct tlc_train {
   void* ws = nullptr;
   Piece* pieces = nullptr;
   double* partials = nullptr;
+  GradWork grad = {};
   // pinned: the sticky index flag and the staging slots of the pieces
   uint32_t* bad = nullptr;
   uint32_t* bad_dev = nullptr;
@@ -188,11 +189,28 @@ TLC_API int tlc_train_create(tlc_train** out, size_t max_tokens, size_t max_rows
     return hip_fail(e, "hipGetDevice");
   }
   c->slot_pieces = max_tensors ? kNormBlocks + max_tensors : 0;
-  // layout: pieces | partial sums
+  // layout: pieces | partial sums | sorted tokens, twice | counts of the sort |
+  //         touched rows | partial rows
   size_t off = round_up(c->slot_pieces * sizeof(Piece), 256);
   const size_t off_partials = off;
   off = round_up(off + kNormBlocks * sizeof(double), 256);
+  size_t off_sort[4], off_counts[3];
+  for (size_t& o : off_sort) {
+    o = off;
+    off = round_up(off + max_tokens * sizeof(uint32_t), 256);
+  }
+  for (size_t& o : off_counts) {
+    o = off;
+    off = round_up(off + ceil_div(max_tokens, kSortTile) * kSortMaxDigits * sizeof(uint32_t), 256);
+  }
+  const size_t off_touched = off;
+  off = round_up(off + max_rows, 256);
+  const size_t off_parts = off;
+  off = round_up(off + ceil_div(max_tokens, kSumMinTokens * kSumWaves) * 2 * max_dim *
+                           sizeof(float), 256);
   e = hipMalloc(&c->ws, off);
+  if (e == hipSuccess) e = hipMemset((uint8_t*)c->ws + off_touched, 0, max_rows);
+  if (e == hipSuccess) e = hipDeviceSynchronize();
   if (e == hipSuccess) e = hipHostMalloc((void**)&c->bad, 256, hipHostMallocDefault);
   if (e == hipSuccess) e = hipHostGetDevicePointer((void**)&c->bad_dev, c->bad, 0);
   if (e == hipSuccess && c->slot_pieces)
@@ -205,8 +223,16 @@ TLC_API int tlc_train_create(tlc_train** out, size_t max_tokens, size_t max_rows
     return hip_fail(e, "tlc_train_create: workspace");
   }
   *c->bad = 0u;
-  c->pieces = (Piece*)c->ws;
-  c->partials = (double*)((uint8_t*)c->ws + off_partials);
+  uint8_t* base = (uint8_t*)c->ws;
+  c->pieces = (Piece*)base;
+  c->partials = (double*)(base + off_partials);
+  for (int i = 0; i < 2; ++i) {
+    c->grad.keys[i] = (uint32_t*)(base + off_sort[i]);
+    c->grad.pos[i] = (uint32_t*)(base + off_sort[2 + i]);
+  }
+  for (int i = 0; i < 3; ++i) c->grad.counts[i] = (uint32_t*)(base + off_counts[i]);
+  c->grad.touched = base + off_touched;
+  c->grad.parts = (float*)(base + off_parts);
   try {
     c->host_pieces.reserve(c->slot_pieces);
     c->spans.reserve(2 * max_tensors + 1);
@@ -326,8 +352,8 @@ TLC_API int tlc_embedding_grad(tlc_train* c, const void* grad, int grad_type, si
   a.scale = scale;
   a.padding = padding_id;
   a.bad = c->bad_dev;
-  return launched(c, launch_embedding_grad(a, grad_type, ids_type, accumulate != 0, c->stream),
-                  fn);
+  return launched(c, launch_embedding_grad(a, grad_type, ids_type, accumulate != 0, c->grad,
+                                           c->stream), fn);
 }
 
 // ---------------------------------------------------------------- norm, clip

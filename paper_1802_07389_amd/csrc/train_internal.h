@@ -4,6 +4,7 @@
 #pragma once
 
 #include "tlc_internal.h"
+#include "typed_io.hpp"
 
 namespace tlc {
 
@@ -23,8 +24,58 @@ struct EmbArgs {
 
 hipError_t launch_embedding(const EmbArgs& a, int table_type, int ids_type, int out_type,
                             hipStream_t st);
+
+// The gradient's sort: tiles of tokens, digits of at most kSortMaxBits of their
+// rows (heights below 2^11 in one pass, below 2^22 in two).
+constexpr uint32_t kSortThreads = 512;
+constexpr uint32_t kSortTile = 2048;
+constexpr uint32_t kSortMaxBits = 11;
+constexpr uint32_t kSortMaxDigits = 1u << kSortMaxBits;
+struct SortArgs {
+  const uint32_t* keys_in;
+  const uint32_t* pos_in;  // NULL: the tokens in their order
+  uint32_t* keys_out;
+  uint32_t* pos_out;
+  const uint32_t* counts;  // per tile and digit
+  uint32_t* next;          // the next pass's counts, or NULL
+  uint32_t count, tiles, shift, bits, next_bits;
+};
+// Zeroes for the rows that no token touches.
+struct FillArgs {
+  float* out;
+  uint64_t out_stride;
+  const uint8_t* touched;
+  uint64_t rows;
+  uint32_t dim, block_rows, block0;
+  Divider packs;  // float4s (or, of shorter rows, floats) of a row
+};
+constexpr uint32_t kFillPacks = 4096;    // of one block
+constexpr uint32_t kFillBeside = 1024;   // blocks of the fill beside a pass of the sort
+// The sums: kSumWaves waves of a block, each per_wave sorted tokens.
+constexpr uint32_t kSumThreads = 256;
+constexpr uint32_t kSumWaves = kSumThreads / 64;
+constexpr uint32_t kSumMinTokens = 16, kSumMaxTokens = 64;  // of a wave
+constexpr uint32_t kJoinThreads = 512;
+struct SumArgs {
+  const uint32_t* keys;  // sorted; `rows` and above: adds nothing
+  const uint32_t* pos;
+  float* parts;          // per block of tokens: head, tail (dim values each)
+  uint32_t packs, slabs, per_wave, blocks;
+};
+inline uint32_t sum_per_wave(uint32_t count, uint32_t slabs) {
+  const uint64_t each = (uint64_t)count * slabs / 4096 / 8 * 8;
+  return (uint32_t)std::min<uint64_t>(std::max<uint64_t>(each, kSumMinTokens), kSumMaxTokens);
+}
+// Device memory of the gradient; touched is zero between calls.
+struct GradWork {
+  uint32_t* keys[2];
+  uint32_t* pos[2];
+  uint32_t* counts[3];
+  uint8_t* touched;
+  float* parts;
+};
 hipError_t launch_embedding_grad(const EmbArgs& a, int grad_type, int ids_type, bool accumulate,
-                                 hipStream_t st);
+                                 const GradWork& w, hipStream_t st);
 
 // A list of tensors is cut into pieces of one length (the last of a tensor
 // shorter).  A block takes consecutive pieces.
