@@ -19,187 +19,208 @@
 namespace tlc {
 namespace {
 
-constexpr int kSortWaves = kSortThreads / 64;
-constexpr int kSortItems = kSortTile / kSortThreads;
+constexpr uint32_t kDigitMask = kDigits - 1;
 
 // The key a token is sorted by: its row, or `rows` (after all others) where it
-// adds nothing.
-template <class Id>
-__device__ __forceinline__ uint32_t token_key(const EmbArgs& a, uint32_t t) {
-  const int64_t id = static_cast<const Id*>(a.ids)[t];
+// adds nothing.  report: an id outside the table sets the call's flag.
+__device__ __forceinline__ uint32_t token_key(const EmbArgs& a, uint32_t t, bool report) {
+  const int64_t id = a.wide_ids ? static_cast<const int64_t*>(a.ids)[t]
+                                : (int64_t)static_cast<const int32_t*>(a.ids)[t];
   if (id >= 0 && id == a.padding) return a.rows;
   if (id < 0 || id >= (int64_t)a.rows) {
-    host_put(a.bad, 1u);
+    if (report) host_put(a.bad, 1u);
     return a.rows;
   }
   return (uint32_t)id;
 }
 
-// Zeroes the rows of block b of the fill that no token touched.
+// Zeroes the rows of block b of the fill that no token touched; touched: marks
+// of the block's rows.
 template <uint32_t kBlock>
-__device__ __forceinline__ void fill_rows(const FillArgs& f, uint32_t b) {
+__device__ __forceinline__ void fill_rows(const FillArgs& f, uint32_t b, const uint8_t* touched) {
   const uint64_t r0 = (uint64_t)b * f.block_rows;
   const uint32_t n = (uint32_t)umin64(f.block_rows, f.rows - r0) * f.packs.d;
   float* out = f.out + r0 * f.out_stride;
   for (uint32_t u = threadIdx.x; u < n; u += kBlock) {
     const uint32_t r = quotient(u, f.packs);
-    if (f.touched[r0 + r]) continue;
+    if (touched[r]) continue;
     float* o = out + r * f.out_stride;
     const uint32_t j = u - r * f.packs.d;
     if (f.dim >= 4)
-      st4(o + umin32(j * 4, f.dim - 4), make_float4(0.0f, 0.0f, 0.0f, 0.0f));
+      st_stream(o + umin32(j * 4, f.dim - 4), make_float4(0.0f, 0.0f, 0.0f, 0.0f));
     else
       o[j] = 0.0f;
   }
 }
 
-}  // namespace
-
-// The keys, the counts of every tile's first digits, and the rows that any
-// token touches (touched NULL: not wanted).  Clears the counts of the passes
-// after the first (next1, next2: may be NULL).
-template <class Id>
-__global__ __launch_bounds__(kSortThreads) void tlc_token_count_kernel(
-    EmbArgs a, uint32_t* __restrict__ keys, uint8_t* __restrict__ touched,
-    uint32_t* __restrict__ counts, uint32_t* __restrict__ next1, uint32_t* __restrict__ next2,
-    uint32_t digits) {
-  __shared__ uint32_t n[kSortMaxDigits];
-  for (uint32_t d = threadIdx.x; d < digits; d += kSortThreads) n[d] = 0u;
-  __syncthreads();
+// The lanes below this one, and those that share its digit among the lanes
+// `in`, from the ballots of the digit's bits.
+__device__ __forceinline__ uint64_t lanes_below() {
+  return ((uint64_t)1 << (threadIdx.x & 63u)) - 1;
+}
+__device__ __forceinline__ uint64_t same_digit(uint32_t d, bool in) {
+  uint64_t same = __ballot(in);
 #pragma unroll
-  for (int i = 0; i < kSortItems; ++i) {
-    const uint32_t t = blockIdx.x * kSortTile + i * kSortThreads + threadIdx.x;
-    if (t >= a.count) break;
-    const uint32_t key = token_key<Id>(a, t);
-    keys[t] = key;
-    if (touched && key < a.rows) touched[key] = 1;
-    atomicAdd(&n[key & (digits - 1)], 1u);
+  for (uint32_t b = 0; b < kDigitBits; ++b) {
+    const uint64_t m = __ballot((d >> b) & 1u);
+    same &= (d >> b) & 1u ? m : ~m;
   }
-  __syncthreads();
-  const uint64_t at = (uint64_t)blockIdx.x * digits;
-  for (uint32_t d = threadIdx.x; d < digits; d += kSortThreads) {
-    counts[at + d] = n[d];
-    if (next1) next1[at + d] = 0u;
-    if (next2) next2[at + d] = 0u;
-  }
+  return same;
 }
 
-// One pass: the tile's keys go where the counts of all tiles send them, those
-// of equal digits in their order.  A wave ranks 64 neighbouring keys at a time
-// by the ballots of their digits' bits.  Counts the next pass's digits (by the
-// tile that a key goes to), one addition for all neighbours that share digit and
-// tile.  Blocks from `tiles` on fill rows instead.
-__global__ __launch_bounds__(kSortThreads) void tlc_token_sort_kernel(SortArgs s, FillArgs f) {
-  __shared__ uint16_t wave_n[kSortWaves][kSortMaxDigits];
-  __shared__ uint32_t base[kSortMaxDigits];
-  __shared__ uint32_t scan_lds[kSortWaves];
-  if (blockIdx.x >= s.tiles) {
-    fill_rows<kSortThreads>(f, f.block0 + blockIdx.x - s.tiles);
-    return;
-  }
-  const uint32_t lane = threadIdx.x & 63u, wid = threadIdx.x >> 6;
-  const uint32_t digits = 1u << s.bits;
-  constexpr uint32_t kPer = kSortMaxDigits / kSortThreads;
-  // where the tile's keys of every digit start
-  uint32_t before[kPer];
+// A wave's rank of its keys among those of equal digit, 64 neighbouring keys at
+// a time; n: the wave's counts, zero before, its keys per digit after.
+template <int kItems>
+__device__ __forceinline__ void rank_keys(const uint32_t (&key)[kItems], uint32_t items,
+                                          uint32_t shift, uint16_t* n, uint32_t (&rank)[kItems]) {
+  const uint64_t below = lanes_below();
 #pragma unroll
-  for (uint32_t i = 0; i < kPer; ++i) {
-    const uint32_t d = threadIdx.x + i * kSortThreads;
-    before[i] = 0;
-    if (d >= digits) break;
-    uint32_t total = 0;
-#pragma unroll 8
-    for (uint32_t t = 0; t < s.tiles; ++t) {
-      const uint32_t v = s.counts[(uint64_t)t * digits + d];
-      before[i] += t < blockIdx.x ? v : 0u;
-      total += v;
-    }
-    base[d] = total;
-#pragma unroll
-    for (int w = 0; w < kSortWaves; ++w) wave_n[w][d] = 0;
-  }
-  __syncthreads();
-  const uint32_t d0 = threadIdx.x * kPer;
-  uint32_t own[kPer], sum = 0;
-#pragma unroll
-  for (uint32_t i = 0; i < kPer; ++i) {
-    own[i] = d0 + i < digits ? base[d0 + i] : 0u;
-    sum += own[i];
-  }
-  uint32_t excl = block_scan_u32<kSortWaves>(sum, scan_lds).excl;
-#pragma unroll
-  for (uint32_t i = 0; i < kPer; ++i) {
-    if (d0 + i < digits) base[d0 + i] = excl;
-    excl += own[i];
-  }
-  // rank within the wave
-  const uint32_t t0 = blockIdx.x * kSortTile + wid * (64 * kSortItems) + lane;
-  uint32_t key[kSortItems], pos[kSortItems], rank[kSortItems];
-#pragma unroll
-  for (int i = 0; i < kSortItems; ++i) {
-    const uint32_t t = t0 + i * 64;
-    key[i] = t < s.count ? s.keys_in[t] : 0u;
-    pos[i] = t < s.count && s.pos_in ? s.pos_in[t] : t;
-  }
-  const uint64_t below = ((uint64_t)1 << lane) - 1;
-#pragma unroll
-  for (int i = 0; i < kSortItems; ++i) {
-    const bool in = t0 + i * 64 < s.count;
-    const uint32_t d = (key[i] >> s.shift) & (digits - 1);
-    uint64_t same = __ballot(in);
-    for (uint32_t b = 0; b < s.bits; ++b) {
-      const uint64_t m = __ballot((d >> b) & 1u);
-      same &= (d >> b) & 1u ? m : ~m;
-    }
-    if (in) rank[i] = wave_n[wid][d] + (uint32_t)__popcll(same & below);
+  for (int i = 0; i < kItems; ++i) {
+    const bool in = i * 64 + (threadIdx.x & 63u) < items;
+    const uint32_t d = (key[i] >> shift) & kDigitMask;
+    const uint64_t same = same_digit(d, in);
+    rank[i] = n[d] + (uint32_t)__popcll(same & below);
     // every lane has read the count before the run's first lane raises it
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    if (in && (same & below) == 0) wave_n[wid][d] += (uint16_t)__popcll(same);
+    if (in && (same & below) == 0) n[d] += (uint16_t)__popcll(same);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   }
+}
+
+// Turns the waves' counts of digit d into their exclusive prefix; returns the sum.
+template <int kW>
+__device__ __forceinline__ uint32_t prefix_waves(uint16_t (*n)[kDigits], uint32_t d) {
+  uint32_t sum = 0;
+#pragma unroll
+  for (int w = 0; w < kW; ++w) {
+    const uint32_t v = n[w][d];
+    n[w][d] = (uint16_t)sum;
+    sum += v;
+  }
+  return sum;
+}
+
+// Sorts 1024 * kItems keys and their numbers within a block, digit by digit.
+template <int kItems>
+__device__ __forceinline__ void sort_block(uint32_t (&key)[kItems], uint32_t passes,
+                                           uint16_t (*wave_n)[kDigits], uint32_t* base,
+                                           uint32_t* scan_lds, uint32_t* keys, uint16_t* poss) {
+  constexpr int kW = kSmallThreads / 64;
+  const uint32_t lane = threadIdx.x & 63u, wid = threadIdx.x >> 6;
+  const uint32_t t0 = wid * (64 * kItems) + lane;
+  uint32_t pos[kItems], rank[kItems];
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) pos[i] = t0 + i * 64;
+  for (uint32_t p = 0; p < passes; ++p) {
+    for (uint32_t i = threadIdx.x; i < kW * kDigits / 2; i += kSmallThreads)
+      reinterpret_cast<uint32_t*>(wave_n)[i] = 0u;
+    __syncthreads();
+    rank_keys<kItems>(key, 64 * kItems, p * kDigitBits, wave_n[wid], rank);
+    __syncthreads();
+    const uint32_t n = threadIdx.x < kDigits ? prefix_waves<kW>(wave_n, threadIdx.x) : 0u;
+    const uint32_t excl = block_scan_u32<kW>(n, scan_lds).excl;
+    if (threadIdx.x < kDigits) base[threadIdx.x] = excl;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      const uint32_t d = (key[i] >> (p * kDigitBits)) & kDigitMask;
+      const uint32_t to = base[d] + wave_n[wid][d] + rank[i];
+      keys[to] = key[i];
+      poss[to] = (uint16_t)pos[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      key[i] = keys[t0 + i * 64];
+      pos[i] = poss[t0 + i * 64];
+    }
+  }
+}
+
+}  // namespace
+
+// The counts of a pass's digits in every tile; the first pass's also makes the
+// keys, and marks the rows that any token touches (touched NULL: not wanted).
+// Blocks from `tiles` on fill rows.
+template <int kItems>
+__global__ __launch_bounds__(kSortThreads) void tlc_token_count_kernel(
+    EmbArgs a, SortArgs s, uint32_t* __restrict__ keys, uint8_t* __restrict__ touched,
+    FillArgs f) {
+  if (blockIdx.x >= s.tiles) {
+    const uint32_t b = f.block0 + blockIdx.x - s.tiles;
+    fill_rows<kSortThreads>(f, b, f.touched + (uint64_t)b * f.block_rows);
+    return;
+  }
+  __shared__ uint32_t n[kDigits];
+  if (threadIdx.x < kDigits) n[threadIdx.x] = 0u;
   __syncthreads();
 #pragma unroll
-  for (uint32_t i = 0; i < kPer; ++i) {
-    const uint32_t d = threadIdx.x + i * kSortThreads;
-    if (d >= digits) break;
-    uint32_t n = 0;
-#pragma unroll
-    for (int w = 0; w < kSortWaves; ++w) {
-      const uint32_t v = wave_n[w][d];
-      wave_n[w][d] = (uint16_t)n;
-      n += v;
+  for (int i = 0; i < kItems; ++i) {
+    const uint32_t t = (blockIdx.x * kItems + i) * kSortThreads + threadIdx.x;
+    if (t >= a.count) break;
+    uint32_t key;
+    if (s.shift == 0) {
+      key = token_key(a, t, true);
+      keys[t] = key;
+      if (touched && key < a.rows) touched[key] = 1;
+    } else {
+      key = s.keys_in[t];
     }
-    base[d] += before[i];
+    atomicAdd(&n[(key >> s.shift) & kDigitMask], 1u);
   }
   __syncthreads();
+  if (threadIdx.x < kDigits) s.counts[blockIdx.x * kDigits + threadIdx.x] = n[threadIdx.x];
+}
+
+// One pass over tiles: a tile's keys go where the counts of all tiles send them,
+// those of equal digits in their order.
+template <int kItems>
+__global__ __launch_bounds__(kSortThreads) void tlc_token_sort_kernel(SortArgs s, FillArgs f) {
+  constexpr int kW = kSortThreads / 64;
+  __shared__ uint16_t wave_n[kW][kDigits];
+  __shared__ uint32_t base[kDigits];
+  __shared__ uint32_t scan_lds[kW];
+  if (blockIdx.x >= s.tiles) {
+    const uint32_t b = f.block0 + blockIdx.x - s.tiles;
+    fill_rows<kSortThreads>(f, b, f.touched + (uint64_t)b * f.block_rows);
+    return;
+  }
+  static_assert(kDigits == kSortThreads, "a digit a thread");
+  const uint32_t lane = threadIdx.x & 63u, wid = threadIdx.x >> 6;
+  const uint32_t t0 = blockIdx.x * (kSortThreads * kItems) + wid * (64 * kItems);
+  const uint32_t items = t0 < s.count ? s.count - t0 : 0u;
+  uint32_t key[kItems], pos[kItems], rank[kItems];
 #pragma unroll
-  for (int i = 0; i < kSortItems; ++i) {
-    const bool in = t0 + i * 64 < s.count;
-    const uint32_t d = (key[i] >> s.shift) & (digits - 1);
-    const uint32_t to = in ? base[d] + wave_n[wid][d] + rank[i] : 0u;
-    if (in) {
-      s.keys_out[to] = key[i];
-      s.pos_out[to] = pos[i];
-    }
-    if (s.next) {
-      const uint32_t nd = (key[i] >> (s.shift + s.bits)) & ((1u << s.next_bits) - 1);
-      // lanes of one digit go to neighbouring places: their tiles differ by
-      // at most one, so that the tile's parity tells them apart
-      const uint32_t word = d | nd << s.bits;
-      uint64_t same = __ballot(in);
-      for (uint32_t b = 0; b < s.bits + s.next_bits; ++b) {
-        const uint64_t m = __ballot((word >> b) & 1u);
-        same &= (word >> b) & 1u ? m : ~m;
-      }
-      const uint32_t odd = (to / kSortTile) & 1u;
-      const uint64_t m = __ballot(odd);
-      same &= odd ? m : ~m;
-      if (in && (same & below) == 0)
-        atomicAdd(&s.next[((uint64_t)(to / kSortTile) << s.next_bits) + nd],
-                  (uint32_t)__popcll(same));
-    }
+  for (int i = 0; i < kItems; ++i) {
+    const uint32_t t = t0 + i * 64 + lane;
+    key[i] = t < s.count ? s.keys_in[t] : 0u;
+    pos[i] = t < s.count && s.pos_in ? s.pos_in[t] : t;
+  }
+#pragma unroll
+  for (int w = 0; w < kW; ++w) wave_n[w][threadIdx.x] = 0;
+  // the digit's keys in the tiles before this one, and in all
+  uint32_t before = 0, total = 0;
+#pragma unroll 16
+  for (uint32_t t = 0; t < s.tiles; ++t) {
+    const uint32_t v = s.counts[t * kDigits + threadIdx.x];
+    before += t < blockIdx.x ? v : 0u;
+    total += v;
+  }
+  __syncthreads();
+  rank_keys<kItems>(key, items, s.shift, wave_n[wid], rank);
+  const uint32_t excl = block_scan_u32<kW>(total, scan_lds).excl;  // and a barrier
+  base[threadIdx.x] = excl + before;
+  prefix_waves<kW>(wave_n, threadIdx.x);
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) {
+    if (i * 64 + lane >= items) break;
+    const uint32_t d = (key[i] >> s.shift) & kDigitMask;
+    const uint32_t to = base[d] + wave_n[wid][d] + rank[i];
+    s.keys_out[to] = key[i];
+    s.pos_out[to] = pos[i];
   }
 }
 
@@ -240,106 +261,203 @@ __device__ __forceinline__ void put_row(const EmbArgs& a, uint32_t row, uint32_t
   store_pack<float, V>(p, o);
 }
 
+// The columns of a lane: packs of V, shared out evenly over the slabs (64 packs
+// at most each); the last pack of a row is moved back to end with it, in the
+// slab of the pack that it overlaps (both lanes load before either stores).
+template <int V>
+struct Columns {
+  bool in;
+  uint32_t k;
+  __device__ __forceinline__ Columns(uint32_t dim, uint32_t packs, uint32_t slabs, uint32_t slab) {
+    const uint32_t lane = threadIdx.x & 63u;
+    const uint32_t p0 = (uint32_t)((uint64_t)slab * packs / slabs);
+    const uint32_t p1 = (uint32_t)((uint64_t)(slab + 1) * packs / slabs);
+    in = p0 + lane < p1;
+    k = umin32((p0 + lane) * V, dim - V);
+  }
+};
+
+// One wave's sorted tokens [c0, c1) of one slab of columns.  Runs are summed
+// eight rows at a time; one that neither began before c0 nor goes on at c1 is
+// final.  A run that began before goes to `head` (the lane's place in LDS);
+// one that goes on is left in sum.
+template <class In, int V>
+struct WaveRuns {
+  Sum<V> sum = {};
+  uint32_t cur = 0;
+  bool first = false, tail = false, any = false;  // any: [c0, c1) has a token that counts
+  uint32_t head = 0;  // 1: ends in the wave, 3: goes on after it
+
+  template <class Pos>
+  __device__ __forceinline__ void run(const EmbArgs& a, const uint32_t* keys, const Pos* poss,
+                                      uint32_t count, uint32_t c0, uint32_t c1, Columns<V> col,
+                                      float* lds_head, bool accumulate) {
+    constexpr int kRows = 8;  // rows in flight
+    const uint32_t lane = threadIdx.x & 63u;
+    const In* x = static_cast<const In*>(a.x) + col.k;
+    const uint32_t prev = c0 > 0 && c0 < c1 ? keys[c0 - 1] : a.rows;
+    const uint32_t next = c1 < count ? keys[c1] : a.rows;
+    for (uint32_t c = c0; c < c1; c += 64) {
+      const uint32_t key = c + lane < c1 ? keys[c + lane] : a.rows;
+      const uint32_t pos = c + lane < c1 ? poss[c + lane] : 0u;
+      const uint32_t n = (uint32_t)__popcll(__ballot(key < a.rows));
+      if (n == 0) break;
+      if (c == c0) {
+        any = true;
+        cur = uniform32(key);
+        first = uniform32(prev) == cur;
+        head = first ? 1u : 0u;
+      }
+      for (uint32_t e = 0; e < n; e += kRows) {
+        Pack<In, V> r[kRows];
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+          const uint32_t t =
+              (uint32_t)__builtin_amdgcn_readlane((int)pos, (int)umin32(e + i, n - 1));
+          if (col.in) r[i] = load_pack<In, V, true>(x + (uint64_t)t * a.x_stride);
+        }
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+          if (e + i >= n) break;
+          const uint32_t row = (uint32_t)__builtin_amdgcn_readlane((int)key, (int)(e + i));
+          if (row != cur) {
+            if (col.in) {
+              if (first)
+                put_floats<V>(lds_head, sum.v);
+              else
+                put_row<V>(a, cur, col.k, sum.v, accumulate);
+            }
+            first = false;
+            cur = row;
+            sum = {};
+          }
+          if (col.in) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) sum.v[j] += r[i].get(j);
+          }
+        }
+      }
+    }
+    const bool on = any && uniform32(next) == cur;
+    tail = on && !first;
+    if (any && col.in) {
+      if (first)
+        put_floats<V>(lds_head, sum.v);
+      else if (!on)
+        put_row<V>(a, cur, col.k, sum.v, accumulate);
+    }
+    if (first && on) head = 3u;
+  }
+
+  // After all waves have run: the wave where a run begins adds the later waves'
+  // parts of it.  False: it goes on past the block.
+  template <int kW>
+  __device__ __forceinline__ bool finish(const EmbArgs& a, const float (*lds)[64 * V],
+                                         const uint32_t* heads, uint32_t wid, Columns<V> col,
+                                         bool accumulate) {
+    bool ends = false;
+    for (uint32_t w = wid + 1; w < kW && !ends; ++w) {
+      if (col.in) sum.add(&lds[w][(threadIdx.x & 63u) * V]);
+      ends = heads[w] == 1u;
+    }
+    if (ends && col.in) put_row<V>(a, cur, col.k, sum.v, accumulate);
+    return ends;
+  }
+};
+
 }  // namespace
 
-// Every wave: `per_wave` sorted tokens (at most 64) of one slab of columns.  Its
-// runs are summed eight rows at a time; one that neither began before the wave
-// nor goes on after it is final.  The others' parts meet in LDS: the wave where a
-// run begins adds the parts of the block's later waves, and leaves the sum as
-// the block's tail if the run goes on in the next block; what the block adds to
-// a run that began earlier is its head.
-template <class In, int V>
-__global__ __launch_bounds__(kSumThreads) void tlc_embedding_grad_sum_kernel(EmbArgs a, SumArgs s,
-                                                                             bool accumulate,
-                                                                             FillArgs f) {
-  constexpr int kRows = 8;  // rows in flight
-  __shared__ float lds[kSumWaves][64 * V];
-  __shared__ uint32_t lds_head[kSumWaves];  // 1: has a head; 2: the run goes on
+// Few tokens in one launch, without a partial row: every block sorts all of
+// them, and takes the runs that begin in its share of the sorted tokens, its
+// waves an equal part each.  Blocks from `blocks` * `slabs` on look at all ids and
+// fill rows.
+template <class In, int V, int kItems>
+__global__ __launch_bounds__(kSmallThreads) void tlc_embedding_grad_small_kernel(
+    EmbArgs a, SumArgs s, bool accumulate, uint32_t passes, FillArgs f) {
+  constexpr int kW = kSmallThreads / 64;
+  constexpr uint32_t kSlots = kSmallThreads * kItems;
+  __shared__ union {
+    uint16_t wave_n[kW][kDigits];  // while the tokens are sorted
+    float heads[kW][64 * V];       // while their rows are summed
+    uint8_t marks[kSmallFillRows];
+  } lds;
+  __shared__ uint32_t keys[kSlots];
+  __shared__ uint16_t poss[kSlots];
+  __shared__ uint32_t base[kDigits];
+  __shared__ uint32_t scan_lds[kW], head[kW], span[2];
+  const uint32_t lane = threadIdx.x & 63u, wid = uniform32(threadIdx.x >> 6);
   if (blockIdx.x >= s.blocks * s.slabs) {
-    fill_rows<kSumThreads>(f, f.block0 + blockIdx.x - s.blocks * s.slabs);
+    const uint32_t b = blockIdx.x - s.blocks * s.slabs;
+    const uint64_t r0 = (uint64_t)b * f.block_rows;
+    for (uint32_t r = threadIdx.x; r < f.block_rows; r += kSmallThreads) lds.marks[r] = 0;
+    __syncthreads();
+    for (uint32_t t = threadIdx.x; t < a.count; t += kSmallThreads) {
+      const uint32_t key = token_key(a, t, false);
+      if (key < a.rows && key - r0 < f.block_rows) lds.marks[key - r0] = 1;
+    }
+    __syncthreads();
+    fill_rows<kSmallThreads>(f, b, lds.marks);
     return;
   }
+  const uint32_t block = blockIdx.x / s.slabs, slab = blockIdx.x % s.slabs;
+  const uint32_t t0 = wid * (64 * kItems) + lane;
+  uint32_t key[kItems];
+#pragma unroll
+  for (int i = 0; i < kItems; ++i)  // slots past the last token sort after all of them
+    key[i] = t0 + i * 64 < a.count ? token_key(a, t0 + i * 64, blockIdx.x == 0) : 0xffffffffu;
+  sort_block<kItems>(key, passes, lds.wave_n, base, scan_lds, keys, poss);
+  // the first run that begins in the share, and the first after it
+  if (threadIdx.x < 2) span[threadIdx.x] = a.count;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) {
+    const uint32_t c = t0 + i * 64;
+    const bool begins = c < a.count && (c == 0 || keys[c - 1] != key[i]);
+#pragma unroll
+    for (uint32_t e = 0; e < 2; ++e) {
+      const uint64_t m = __ballot(begins && c >= (block + e) * s.per_wave);
+      if (m && lane == 0) atomicMin(&span[e], c + (uint32_t)__builtin_ctzll(m));
+    }
+  }
+  __syncthreads();
+  const uint32_t s0 = uniform32(span[0]), s1 = uniform32(span[1]);
+  const uint32_t per = umax32((s1 - s0 + kW - 1) / kW, 4u);
+  const uint32_t c0 = umin32(s0 + wid * per, s1), c1 = umin32(c0 + per, s1);
+  const Columns<V> col(a.dim, s.packs, s.slabs, slab);
+  WaveRuns<In, V> runs;
+  runs.run(a, keys, poss, a.count, c0, c1, col, &lds.heads[wid][lane * V], accumulate);
+  if (lane == 0) head[wid] = runs.head;
+  __syncthreads();
+  if (runs.tail) runs.template finish<kW>(a, lds.heads, head, wid, col, accumulate);
+}
+
+// Every wave: `per_wave` sorted tokens of one slab of columns.  What the block
+// adds to a run that began earlier is its head, what it has of one that goes
+// on its tail: partial rows for the join.
+template <class In, int V>
+__global__ __launch_bounds__(kSumThreads) void tlc_embedding_grad_sum_kernel(EmbArgs a, SumArgs s,
+                                                                             bool accumulate) {
+  __shared__ float lds[kSumWaves][64 * V];
+  __shared__ uint32_t head[kSumWaves];
   const uint32_t lane = threadIdx.x & 63u, wid = uniform32(threadIdx.x >> 6);
   const uint32_t block = blockIdx.x / s.slabs, slab = blockIdx.x % s.slabs;
-  // packs of the slab; the last of a row is moved back to end with it, beside
-  // the pack that it overlaps (both lanes load before either stores)
-  const uint32_t p0 = (uint32_t)((uint64_t)slab * s.packs / s.slabs);
-  const uint32_t p1 = (uint32_t)((uint64_t)(slab + 1) * s.packs / s.slabs);
-  const bool in = p0 + lane < p1;
-  const uint32_t k = umin32((p0 + lane) * V, a.dim - V);
+  const Columns<V> col(a.dim, s.packs, s.slabs, slab);
   const uint32_t c0 = umin32((block * kSumWaves + wid) * s.per_wave, a.count);
   const uint32_t c1 = umin32(c0 + s.per_wave, a.count);
-  const uint32_t key = c0 + lane < c1 ? s.keys[c0 + lane] : a.rows;
-  const uint32_t pos = c0 + lane < c1 ? s.pos[c0 + lane] : 0u;
-  const uint32_t prev = c0 > 0 && c0 < c1 ? s.keys[c0 - 1] : a.rows;
-  const uint32_t next = c1 < a.count ? s.keys[c1] : a.rows;
-  const uint32_t n = (uint32_t)__popcll(__ballot(key < a.rows));
-  const In* x = static_cast<const In*>(a.x) + k;
-  Sum<V> sum = {};
-  uint32_t cur = uniform32(key);
-  bool first = n > 0 && uniform32(prev) == cur;  // the run began before
-  uint32_t head = first ? 1u : 0u;
-  for (uint32_t e = 0; e < n; e += kRows) {
-    Pack<In, V> r[kRows];
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      const uint32_t t =
-          (uint32_t)__builtin_amdgcn_readlane((int)pos, (int)umin32(e + i, n - 1));
-      if (in) r[i] = load_pack<In, V>(x + (uint64_t)t * a.x_stride);
-    }
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      if (e + i >= n) break;
-      const uint32_t row = (uint32_t)__builtin_amdgcn_readlane((int)key, (int)(e + i));
-      if (row != cur) {
-        if (in) {
-          if (first)
-            put_floats<V>(&lds[wid][lane * V], sum.v);
-          else
-            put_row<V>(a, cur, k, sum.v, accumulate);
-        }
-        first = false;
-        cur = row;
-        sum = {};
-      }
-      if (in) {
-#pragma unroll
-        for (int c = 0; c < V; ++c) sum.v[c] += r[i].get(c);
-      }
-    }
-  }
-  const bool on = n > 0 && uniform32(next) == cur;
-  const bool tail = on && !first;
-  if (n > 0 && in) {
-    if (first)
-      put_floats<V>(&lds[wid][lane * V], sum.v);
-    else if (!on)
-      put_row<V>(a, cur, k, sum.v, accumulate);
-  }
-  if (first && on) head = 3u;
-  if (lane == 0) lds_head[wid] = head;
+  WaveRuns<In, V> runs;
+  runs.run(a, s.keys, s.pos, a.count, c0, c1, col, &lds[wid][lane * V], accumulate);
+  if (lane == 0) head[wid] = runs.head;
   __syncthreads();
-  float* parts = s.parts + (uint64_t)block * 2 * a.dim + k;
-  if (tail) {
-    bool ends = false;
-    for (uint32_t w = wid + 1; w < kSumWaves && !ends; ++w) {
-      if (in) sum.add(&lds[w][lane * V]);
-      ends = lds_head[w] == 1u;
-    }
-    if (in) {
-      if (ends)
-        put_row<V>(a, cur, k, sum.v, accumulate);
-      else
-        put_floats<V>(parts + a.dim, sum.v);
-    }
-  }
-  if (wid == 0 && lds_head[0]) {
-    sum = {};
+  float* parts = s.parts + (uint64_t)block * 2 * a.dim + col.k;
+  if (runs.tail && !runs.template finish<kSumWaves>(a, lds, head, wid, col, accumulate) && col.in)
+    put_floats<V>(parts + a.dim, runs.sum.v);
+  if (wid == 0 && head[0]) {
+    Sum<V> sum = {};
     uint32_t w = 0;
     do {
-      if (in) sum.add(&lds[w][lane * V]);
-    } while (lds_head[w] == 3u && ++w < kSumWaves);
-    if (in) put_floats<V>(parts, sum.v);
+      if (col.in) sum.add(&lds[w][lane * V]);
+    } while (head[w] == 3u && ++w < kSumWaves);
+    if (col.in) put_floats<V>(parts, sum.v);
   }
 }
 
@@ -377,13 +495,10 @@ __global__ __launch_bounds__(kJoinThreads) void tlc_embedding_grad_join_kernel(
   const uint32_t i0 = umin32(wid * per, n), i1 = umin32(i0 + per, n);
   const uint32_t packs = (a.dim + V - 1) / V, slabs = (packs + 63) / 64;
   for (uint32_t slab = blockIdx.y; slab < slabs; slab += gridDim.y) {
-    const uint32_t p0 = (uint32_t)((uint64_t)slab * packs / slabs);
-    const uint32_t p1 = (uint32_t)((uint64_t)(slab + 1) * packs / slabs);
-    const bool in = p0 + lane < p1;
-    const uint32_t k = umin32((p0 + lane) * V, a.dim - V);
-    const float* parts = s.parts + (uint64_t)blockIdx.x * 2 * a.dim + k;
+    const Columns<V> col(a.dim, packs, slabs, slab);
+    const float* parts = s.parts + (uint64_t)blockIdx.x * 2 * a.dim + col.k;
     Sum<V> sum = {};
-    if (in) {
+    if (col.in) {
       for (uint32_t i = i0; i < i1; i += kParts) {
         Pack<float, V> r[kParts];
 #pragma unroll
@@ -400,9 +515,9 @@ __global__ __launch_bounds__(kJoinThreads) void tlc_embedding_grad_join_kernel(
       put_floats<V>(&lds[wid][lane * V], sum.v);
     }
     __syncthreads();
-    if (wid == 0 && in) {
+    if (wid == 0 && col.in) {
       for (uint32_t w = 1; w < kWavesJ && w * per < n; ++w) sum.add(&lds[w][lane * V]);
-      put_row<V>(a, row, k, sum.v, accumulate);
+      put_row<V>(a, row, col.k, sum.v, accumulate);
     }
     __syncthreads();
   }
@@ -410,19 +525,48 @@ __global__ __launch_bounds__(kJoinThreads) void tlc_embedding_grad_join_kernel(
 
 namespace {
 
-template <class In, int V>
-void launch_sum(const EmbArgs& a, SumArgs s, bool accumulate, const FillArgs& f, uint32_t fill,
-                hipStream_t st) {
-  launch_k(tlc_embedding_grad_sum_kernel<In, V>, s.blocks * s.slabs + fill, kSumThreads, st, a, s,
-           accumulate, f);
+// Blocks of the fill for one launch: out of those that are left, a share.
+uint32_t take_fill(FillArgs* f, uint32_t* left, uint32_t launches) {
+  const uint32_t n = *left / launches;
+  f->block0 = f->blocks - *left;
+  *left -= n;
+  return n;
 }
 
-}  // namespace
+// Sorts the tokens, and fills beside; returns which of w.keys and w.pos hold
+// them.
+template <int kItems>
+int sort_tokens(const EmbArgs& a, const GradWork& w, uint32_t passes, FillArgs f, hipStream_t st) {
+  constexpr uint32_t kTile = kSortThreads * kItems;
+  SortArgs s = {};
+  s.count = a.count;
+  s.tiles = (a.count + kTile - 1) / kTile;
+  s.counts = w.counts;
+  uint8_t* touched = f.blocks ? w.touched : nullptr;
+  uint32_t left = f.blocks;
+  for (uint32_t p = 0; p < passes; ++p) {
+    s.keys_in = w.keys[p & 1];
+    s.pos_in = p ? w.pos[p & 1] : nullptr;
+    s.keys_out = w.keys[(p + 1) & 1];
+    s.pos_out = w.pos[(p + 1) & 1];
+    s.shift = p * kDigitBits;
+    // no fill beside the first count, which makes the marks
+    uint32_t fill = p ? take_fill(&f, &left, 2 * (passes - p)) : 0;
+    launch_k(tlc_token_count_kernel<kItems>, s.tiles + fill, kSortThreads, st, a, s, w.keys[0],
+             touched, f);
+    fill = take_fill(&f, &left, 2 * (passes - p) - 1);
+    launch_k(tlc_token_sort_kernel<kItems>, s.tiles + fill, kSortThreads, st, s, f);
+  }
+  return passes & 1;
+}
 
-hipError_t launch_embedding_grad(const EmbArgs& a, int grad_type, int ids_type, bool accumulate,
-                                 const GradWork& w, hipStream_t st) {
+template <class In, int V>
+void launch_grad(const EmbArgs& a, bool accumulate, const GradWork& w, hipStream_t st) {
+  // passes over the bits of 0 .. rows
+  const uint32_t bits = 32 - (uint32_t)__builtin_clz(a.rows);
+  const uint32_t passes = (bits + kDigitBits - 1) / kDigitBits;
+  const bool small = a.count <= kSmallTokens;
   FillArgs f = {};
-  uint32_t fill = 0;  // blocks that zero rows
   if (!accumulate) {
     const uint32_t packs = a.dim >= 4 ? (a.dim + 3) / 4 : a.dim;
     f.out = static_cast<float*>(a.out);
@@ -432,70 +576,55 @@ hipError_t launch_embedding_grad(const EmbArgs& a, int grad_type, int ids_type, 
     f.dim = a.dim;
     f.packs = divider(packs);
     f.block_rows = std::max(1u, kFillPacks / packs);
-    fill = (a.rows + f.block_rows - 1) / f.block_rows;
+    if (small)  // a block looks at all ids: at most about kSmallFillBlocks of them
+      f.block_rows = std::min(std::max(f.block_rows, a.rows / kSmallFillBlocks), kSmallFillRows);
+    f.blocks = (a.rows + f.block_rows - 1) / f.block_rows;
   }
-  // passes of equal digits over the bits of 0 .. rows
-  const uint32_t bits = 32 - (uint32_t)__builtin_clz(a.rows);
-  const uint32_t passes = (bits + kSortMaxBits - 1) / kSortMaxBits;
-  const uint32_t digit = (bits + passes - 1) / passes;
-  const uint32_t tiles = (a.count + kSortTile - 1) / kSortTile;
-  if (tiles) {
-    uint8_t* touched = accumulate ? nullptr : w.touched;
-    uint32_t* next1 = passes > 1 ? w.counts[1] : nullptr;
-    uint32_t* next2 = passes > 2 ? w.counts[2] : nullptr;
-    if (ids_type == TLC_I64)
-      launch_k(tlc_token_count_kernel<int64_t>, tiles, kSortThreads, st, a, w.keys[0], touched,
-               w.counts[0], next1, next2, 1u << digit);
-    else
-      launch_k(tlc_token_count_kernel<int32_t>, tiles, kSortThreads, st, a, w.keys[0], touched,
-               w.counts[0], next1, next2, 1u << digit);
-  }
-  for (uint32_t p = 0; p < passes; ++p) {
-    SortArgs s = {};
-    s.keys_in = w.keys[p & 1];
-    s.pos_in = p ? w.pos[p & 1] : nullptr;
-    s.keys_out = w.keys[(p + 1) & 1];
-    s.pos_out = w.pos[(p + 1) & 1];
-    s.counts = w.counts[p];
-    s.next = p + 1 < passes ? w.counts[p + 1] : nullptr;
-    s.count = a.count;
-    s.tiles = tiles;
-    s.shift = p * digit;
-    s.bits = digit;
-    s.next_bits = digit;
-    // the rest of the fill goes beside the last pass where no sums follow
-    const uint32_t beside = tiles ? std::min(fill, kFillBeside) : fill;
-    if (tiles + beside) launch_k(tlc_token_sort_kernel, tiles + beside, kSortThreads, st, s, f);
-    f.block0 += beside;
-    fill -= beside;
-  }
-  if (tiles == 0) return hipGetLastError();
   SumArgs s = {};
-  s.keys = w.keys[passes & 1];
-  s.pos = w.pos[passes & 1];
   s.parts = w.parts;
-  const uint32_t pack = grad_type == TLC_F32 ? 4 : 8;
-  s.packs = a.dim >= pack ? (a.dim + pack - 1) / pack : a.dim;
+  s.packs = (a.dim + V - 1) / V;
   s.slabs = (s.packs + 63) / 64;
+  if (small) {
+    // about a block for every CU, of eight tokens at least
+    s.per_wave = std::max(8u, (uint32_t)((uint64_t)a.count * s.slabs / kCus));
+    s.blocks = (a.count + s.per_wave - 1) / s.per_wave;
+    const uint32_t grid = s.blocks * s.slabs + f.blocks;
+    if (a.count <= kSmallThreads)
+      launch_k(tlc_embedding_grad_small_kernel<In, V, 1>, grid, kSmallThreads, st, a, s,
+               accumulate, passes, f);
+    else
+      launch_k(tlc_embedding_grad_small_kernel<In, V, 4>, grid, kSmallThreads, st, a, s,
+               accumulate, passes, f);
+    return;
+  }
+  const int at = a.count > kWideTileTokens ? sort_tokens<16>(a, w, passes, f, st)
+                                           : sort_tokens<4>(a, w, passes, f, st);
+  s.keys = w.keys[at];
+  s.pos = w.pos[at];
   s.per_wave = sum_per_wave(a.count, s.slabs);
   s.blocks = (a.count + s.per_wave * kSumWaves - 1) / (s.per_wave * kSumWaves);
+  launch_k(tlc_embedding_grad_sum_kernel<In, V>, s.blocks * s.slabs, kSumThreads, st, a, s,
+           accumulate);
+  uint8_t* touched = accumulate ? nullptr : w.touched;
+  if (a.dim >= 4)
+    launch_k(tlc_embedding_grad_join_kernel<4>, dim3(s.blocks, std::min((a.dim + 255) / 256, 8u)),
+             kJoinThreads, st, a, s, accumulate, touched);
+  else
+    launch_k(tlc_embedding_grad_join_kernel<1>, dim3(s.blocks, 1), kJoinThreads, st, a, s,
+             accumulate, touched);
+}
+
+}  // namespace
+
+hipError_t launch_embedding_grad(const EmbArgs& a, int grad_type, bool accumulate,
+                                 const GradWork& w, hipStream_t st) {
   with_type(grad_type, [&](auto in) {
     using In = decltype(in);
     if (a.dim >= 16 / sizeof(In))
-      launch_sum<In, 16 / sizeof(In)>(a, s, accumulate, f, fill, st);
+      launch_grad<In, 16 / sizeof(In)>(a, accumulate, w, st);
     else
-      launch_sum<In, 1>(a, s, accumulate, f, fill, st);
+      launch_grad<In, 1>(a, accumulate, w, st);
   });
-  uint8_t* touched = accumulate ? nullptr : w.touched;
-  if (s.blocks > 1 || touched) {
-    if (a.dim >= 4)
-      launch_k(tlc_embedding_grad_join_kernel<4>,
-               dim3(s.blocks, std::min((a.dim + 255) / 256, 8u)), kJoinThreads, st, a, s,
-               accumulate, touched);
-    else
-      launch_k(tlc_embedding_grad_join_kernel<1>, dim3(s.blocks, 1), kJoinThreads, st, a, s,
-               accumulate, touched);
-  }
   return hipGetLastError();
 }
 

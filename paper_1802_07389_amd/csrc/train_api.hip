@@ -194,15 +194,13 @@ TLC_API int tlc_train_create(tlc_train** out, size_t max_tokens, size_t max_rows
   size_t off = round_up(c->slot_pieces * sizeof(Piece), 256);
   const size_t off_partials = off;
   off = round_up(off + kNormBlocks * sizeof(double), 256);
-  size_t off_sort[4], off_counts[3];
+  size_t off_sort[4];
   for (size_t& o : off_sort) {
     o = off;
     off = round_up(off + max_tokens * sizeof(uint32_t), 256);
   }
-  for (size_t& o : off_counts) {
-    o = off;
-    off = round_up(off + ceil_div(max_tokens, kSortTile) * kSortMaxDigits * sizeof(uint32_t), 256);
-  }
+  const size_t off_counts = off;
+  off = round_up(off + ceil_div(max_tokens, kSortTile) * kDigits * sizeof(uint32_t), 256);
   const size_t off_touched = off;
   off = round_up(off + max_rows, 256);
   const size_t off_parts = off;
@@ -230,7 +228,7 @@ TLC_API int tlc_train_create(tlc_train** out, size_t max_tokens, size_t max_rows
     c->grad.keys[i] = (uint32_t*)(base + off_sort[i]);
     c->grad.pos[i] = (uint32_t*)(base + off_sort[2 + i]);
   }
-  for (int i = 0; i < 3; ++i) c->grad.counts[i] = (uint32_t*)(base + off_counts[i]);
+  c->grad.counts = (uint32_t*)(base + off_counts);
   c->grad.touched = base + off_touched;
   c->grad.parts = (float*)(base + off_parts);
   try {
@@ -351,8 +349,9 @@ TLC_API int tlc_embedding_grad(tlc_train* c, const void* grad, int grad_type, si
   a.dim = (uint32_t)dim;
   a.scale = scale;
   a.padding = padding_id;
+  a.wide_ids = ids_type == TLC_I64;
   a.bad = c->bad_dev;
-  return launched(c, launch_embedding_grad(a, grad_type, ids_type, accumulate != 0, c->grad,
+  return launched(c, launch_embedding_grad(a, grad_type, accumulate != 0, c->grad,
                                            c->stream), fn);
 }
 

@@ -19,26 +19,31 @@ struct EmbArgs {
   uint32_t count, rows, dim;
   float scale;
   int64_t padding;    // gradient: tokens of this id add nothing
+  bool wide_ids;      // gradient: ids are int64
   uint32_t* bad;      // pinned host word: set where an id is outside the table
 };
 
 hipError_t launch_embedding(const EmbArgs& a, int table_type, int ids_type, int out_type,
                             hipStream_t st);
 
-// The gradient's sort: tiles of tokens, digits of at most kSortMaxBits of their
-// rows (heights below 2^11 in one pass, below 2^22 in two).
+// The gradient's sort by digits of the tokens' rows (heights below 2^18 in two
+// passes).  Up to kSmallTokens tokens every block of the sums sorts them in LDS;
+// more are sorted first, in tiles of four tokens a thread, above kWideTileTokens
+// of sixteen (every tile's block reads the counts of all).
+constexpr uint32_t kDigitBits = 9;
+constexpr uint32_t kDigits = 1u << kDigitBits;
 constexpr uint32_t kSortThreads = 512;
-constexpr uint32_t kSortTile = 2048;
-constexpr uint32_t kSortMaxBits = 11;
-constexpr uint32_t kSortMaxDigits = 1u << kSortMaxBits;
+constexpr uint32_t kSortTile = kSortThreads * 4;
+constexpr uint32_t kSmallThreads = 1024;
+constexpr uint32_t kSmallTokens = kSmallThreads * 4;
+constexpr uint32_t kWideTileTokens = 1u << 18;
 struct SortArgs {
   const uint32_t* keys_in;
   const uint32_t* pos_in;  // NULL: the tokens in their order
   uint32_t* keys_out;
   uint32_t* pos_out;
-  const uint32_t* counts;  // per tile and digit
-  uint32_t* next;          // the next pass's counts, or NULL
-  uint32_t count, tiles, shift, bits, next_bits;
+  uint32_t* counts;  // per tile and digit
+  uint32_t count, tiles, shift;
 };
 // Zeroes for the rows that no token touches.
 struct FillArgs {
@@ -46,11 +51,12 @@ struct FillArgs {
   uint64_t out_stride;
   const uint8_t* touched;
   uint64_t rows;
-  uint32_t dim, block_rows, block0;
+  uint32_t dim, block_rows, block0, blocks;
   Divider packs;  // float4s (or, of shorter rows, floats) of a row
 };
-constexpr uint32_t kFillPacks = 4096;    // of one block
-constexpr uint32_t kFillBeside = 1024;   // blocks of the fill beside a pass of the sort
+constexpr uint32_t kFillPacks = 4096;  // of one block
+constexpr uint32_t kSmallFillBlocks = 1024;
+constexpr uint32_t kSmallFillRows = 8192;
 // The sums: kSumWaves waves of a block, each per_wave sorted tokens.
 constexpr uint32_t kSumThreads = 256;
 constexpr uint32_t kSumWaves = kSumThreads / 64;
@@ -60,7 +66,8 @@ struct SumArgs {
   const uint32_t* keys;  // sorted; `rows` and above: adds nothing
   const uint32_t* pos;
   float* parts;          // per block of tokens: head, tail (dim values each)
-  uint32_t packs, slabs, per_wave, blocks;
+  uint32_t packs, slabs, blocks;
+  uint32_t per_wave;     // sorted tokens (few tokens: of a block)
 };
 inline uint32_t sum_per_wave(uint32_t count, uint32_t slabs) {
   const uint64_t each = (uint64_t)count * slabs / 4096 / 8 * 8;
@@ -70,11 +77,11 @@ inline uint32_t sum_per_wave(uint32_t count, uint32_t slabs) {
 struct GradWork {
   uint32_t* keys[2];
   uint32_t* pos[2];
-  uint32_t* counts[3];
+  uint32_t* counts;
   uint8_t* touched;
   float* parts;
 };
-hipError_t launch_embedding_grad(const EmbArgs& a, int grad_type, int ids_type, bool accumulate,
+hipError_t launch_embedding_grad(const EmbArgs& a, int grad_type, bool accumulate,
                                  const GradWork& w, hipStream_t st);
 
 // A list of tensors is cut into pieces of one length (the last of a tensor
