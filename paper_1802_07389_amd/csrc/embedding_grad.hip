@@ -41,15 +41,25 @@ __device__ __forceinline__ void fill_rows(const FillArgs& f, uint32_t b, const u
   const uint64_t r0 = (uint64_t)b * f.block_rows;
   const uint32_t n = (uint32_t)umin64(f.block_rows, f.rows - r0) * f.packs.d;
   float* out = f.out + r0 * f.out_stride;
-  for (uint32_t u = threadIdx.x; u < n; u += kBlock) {
-    const uint32_t r = quotient(u, f.packs);
-    if (touched[r]) continue;
-    float* o = out + r * f.out_stride;
-    const uint32_t j = u - r * f.packs.d;
-    if (f.dim >= 4)
-      st_stream(o + umin32(j * 4, f.dim - 4), make_float4(0.0f, 0.0f, 0.0f, 0.0f));
-    else
-      o[j] = 0.0f;
+  constexpr uint32_t kMany = 8;  // marks asked for before the first store
+  for (uint32_t u0 = threadIdx.x; u0 < n; u0 += kMany * kBlock) {
+    uint32_t r[kMany];
+    bool skip[kMany];
+#pragma unroll
+    for (uint32_t i = 0; i < kMany; ++i) {
+      r[i] = quotient(umin32(u0 + i * kBlock, n - 1), f.packs);
+      skip[i] = touched[r[i]] || u0 + i * kBlock >= n;
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kMany; ++i) {
+      if (skip[i]) continue;
+      float* o = out + r[i] * f.out_stride;
+      const uint32_t j = u0 + i * kBlock - r[i] * f.packs.d;
+      if (f.dim >= 4)
+        st_stream(o + umin32(j * 4, f.dim - 4), make_float4(0.0f, 0.0f, 0.0f, 0.0f));
+      else
+        o[j] = 0.0f;
+    }
   }
 }
 
@@ -244,21 +254,26 @@ __device__ __forceinline__ void put_floats(float* p, const float* v) {
   store_pack<float, V>(p, o);
 }
 
-// A row's final values: the scale once, on the whole sum.
+// A row's final values: the scale once, on the whole sum, which is added to
+// what the row holds (kAdd).
 template <int V>
-__device__ __forceinline__ void put_row(const EmbArgs& a, uint32_t row, uint32_t k, const float* v,
-                                        bool accumulate) {
-  float* p = static_cast<float*>(a.out) + row * a.out_stride + k;
-  Pack<float, V> o;
-  if (accumulate) {
-    o = load_pack<float, V>(p);
+__device__ __forceinline__ float* row_at(const EmbArgs& a, uint32_t row, uint32_t k) {
+  return static_cast<float*>(a.out) + (uint64_t)row * a.out_stride + k;
+}
+template <int V, bool kAdd>
+__device__ __forceinline__ void put_row_over(const EmbArgs& a, float* p, Pack<float, V> o,
+                                             const float* v) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) o.set(i, o.get(i) + a.scale * v[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < V; ++i) o.set(i, a.scale * v[i]);
-  }
+  for (int i = 0; i < V; ++i) o.set(i, kAdd ? o.get(i) + a.scale * v[i] : a.scale * v[i]);
   store_pack<float, V>(p, o);
+}
+template <int V, bool kAdd>
+__device__ __forceinline__ void put_row(const EmbArgs& a, uint32_t row, uint32_t k,
+                                        const float* v) {
+  float* p = row_at<V>(a, row, k);
+  Pack<float, V> o = {};
+  if constexpr (kAdd) o = load_pack<float, V>(p);
+  put_row_over<V, kAdd>(a, p, o, v);
 }
 
 // The columns of a lane: packs of V, shared out evenly over the slabs (64 packs
@@ -281,7 +296,7 @@ struct Columns {
 // eight rows at a time; one that neither began before c0 nor goes on at c1 is
 // final.  A run that began before goes to `head` (the lane's place in LDS);
 // one that goes on is left in sum.
-template <class In, int V>
+template <class In, int V, bool kAdd>
 struct WaveRuns {
   Sum<V> sum = {};
   uint32_t cur = 0;
@@ -291,76 +306,83 @@ struct WaveRuns {
   template <class Pos>
   __device__ __forceinline__ void run(const EmbArgs& a, const uint32_t* keys, const Pos* poss,
                                       uint32_t count, uint32_t c0, uint32_t c1, Columns<V> col,
-                                      float* lds_head, bool accumulate) {
+                                      float* lds_head) {
     constexpr int kRows = 8;  // rows in flight
     const uint32_t lane = threadIdx.x & 63u;
-    const In* x = static_cast<const In*>(a.x) + col.k;
     const uint32_t prev = c0 > 0 && c0 < c1 ? keys[c0 - 1] : a.rows;
-    const uint32_t next = c1 < count ? keys[c1] : a.rows;
+    uint32_t next = a.rows;
     for (uint32_t c = c0; c < c1; c += 64) {
       const uint32_t key = c + lane < c1 ? keys[c + lane] : a.rows;
       const uint32_t pos = c + lane < c1 ? poss[c + lane] : 0u;
+      const uint32_t after = c + lane + 1 < count && c + lane < c1 ? keys[c + lane + 1] : a.rows;
       const uint32_t n = (uint32_t)__popcll(__ballot(key < a.rows));
       if (n == 0) break;
+      // the tokens that their runs end with
+      const uint64_t ends = __ballot(key < a.rows && key != after);
       if (c == c0) {
         any = true;
-        cur = uniform32(key);
-        first = uniform32(prev) == cur;
+        first = uniform32(prev) == uniform32(key);
         head = first ? 1u : 0u;
       }
       for (uint32_t e = 0; e < n; e += kRows) {
+        // No lane and no row is left out of the loads (the spare ones repeat the
+        // last): a load under a condition would be waited for before the next
+        // one is asked for.  What the rows hold already is asked for with them.
         Pack<In, V> r[kRows];
+        Pack<float, V> old[kRows];
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-          const uint32_t t =
-              (uint32_t)__builtin_amdgcn_readlane((int)pos, (int)umin32(e + i, n - 1));
-          if (col.in) r[i] = load_pack<In, V, true>(x + (uint64_t)t * a.x_stride);
+          const int at = (int)umin32(e + i, n - 1);
+          const uint32_t t = (uint32_t)__builtin_amdgcn_readlane((int)pos, at);
+          r[i] = load_pack<In, V, true>(static_cast<const In*>(a.x) + t * a.x_stride + col.k);
+          if constexpr (kAdd)
+            old[i] = load_pack<float, V>(
+                row_at<V>(a, (uint32_t)__builtin_amdgcn_readlane((int)key, at), col.k));
+        }
+        if (e + kRows > n) {
+#pragma unroll
+          for (int i = 0; i < kRows; ++i)
+            if (e + i >= n) r[i] = {};
         }
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-          if (e + i >= n) break;
-          const uint32_t row = (uint32_t)__builtin_amdgcn_readlane((int)key, (int)(e + i));
-          if (row != cur) {
+#pragma unroll
+          for (int j = 0; j < V; ++j) sum.v[j] += r[i].get(j);
+          if ((ends >> (e + i)) & 1u) {
+            const uint32_t row = (uint32_t)__builtin_amdgcn_readlane((int)key, (int)(e + i));
             if (col.in) {
               if (first)
                 put_floats<V>(lds_head, sum.v);
               else
-                put_row<V>(a, cur, col.k, sum.v, accumulate);
+                put_row_over<V, kAdd>(a, row_at<V>(a, row, col.k), old[i], sum.v);
             }
             first = false;
-            cur = row;
             sum = {};
-          }
-          if (col.in) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) sum.v[j] += r[i].get(j);
           }
         }
       }
+      cur = (uint32_t)__builtin_amdgcn_readlane((int)key, (int)(n - 1));
+      next = (uint32_t)__builtin_amdgcn_readlane((int)after, (int)(n - 1));
     }
-    const bool on = any && uniform32(next) == cur;
+    const bool on = any && next == cur;  // the last run goes on
     tail = on && !first;
-    if (any && col.in) {
-      if (first)
-        put_floats<V>(lds_head, sum.v);
-      else if (!on)
-        put_row<V>(a, cur, col.k, sum.v, accumulate);
+    if (first && on) {
+      if (col.in) put_floats<V>(lds_head, sum.v);
+      head = 3u;
     }
-    if (first && on) head = 3u;
   }
 
   // After all waves have run: the wave where a run begins adds the later waves'
   // parts of it.  False: it goes on past the block.
   template <int kW>
   __device__ __forceinline__ bool finish(const EmbArgs& a, const float (*lds)[64 * V],
-                                         const uint32_t* heads, uint32_t wid, Columns<V> col,
-                                         bool accumulate) {
+                                         const uint32_t* heads, uint32_t wid, Columns<V> col) {
     bool ends = false;
     for (uint32_t w = wid + 1; w < kW && !ends; ++w) {
       if (col.in) sum.add(&lds[w][(threadIdx.x & 63u) * V]);
       ends = heads[w] == 1u;
     }
-    if (ends && col.in) put_row<V>(a, cur, col.k, sum.v, accumulate);
+    if (ends && col.in) put_row<V, kAdd>(a, cur, col.k, sum.v);
     return ends;
   }
 };
@@ -371,9 +393,9 @@ struct WaveRuns {
 // them, and takes the runs that begin in its share of the sorted tokens, its
 // waves an equal part each.  Blocks from `blocks` * `slabs` on look at all ids and
 // fill rows.
-template <class In, int V, int kItems>
+template <class In, int V, bool kAdd, int kItems>
 __global__ __launch_bounds__(kSmallThreads) void tlc_embedding_grad_small_kernel(
-    EmbArgs a, SumArgs s, bool accumulate, uint32_t passes, FillArgs f) {
+    EmbArgs a, SumArgs s, uint32_t passes, FillArgs f) {
   constexpr int kW = kSmallThreads / 64;
   constexpr uint32_t kSlots = kSmallThreads * kItems;
   __shared__ union {
@@ -424,19 +446,19 @@ __global__ __launch_bounds__(kSmallThreads) void tlc_embedding_grad_small_kernel
   const uint32_t per = umax32((s1 - s0 + kW - 1) / kW, 4u);
   const uint32_t c0 = umin32(s0 + wid * per, s1), c1 = umin32(c0 + per, s1);
   const Columns<V> col(a.dim, s.packs, s.slabs, slab);
-  WaveRuns<In, V> runs;
-  runs.run(a, keys, poss, a.count, c0, c1, col, &lds.heads[wid][lane * V], accumulate);
+  WaveRuns<In, V, kAdd> runs;
+  runs.run(a, keys, poss, a.count, c0, c1, col, &lds.heads[wid][lane * V]);
   if (lane == 0) head[wid] = runs.head;
   __syncthreads();
-  if (runs.tail) runs.template finish<kW>(a, lds.heads, head, wid, col, accumulate);
+  if (runs.tail) runs.template finish<kW>(a, lds.heads, head, wid, col);
 }
 
 // Every wave: `per_wave` sorted tokens of one slab of columns.  What the block
 // adds to a run that began earlier is its head, what it has of one that goes
 // on its tail: partial rows for the join.
-template <class In, int V>
-__global__ __launch_bounds__(kSumThreads) void tlc_embedding_grad_sum_kernel(EmbArgs a, SumArgs s,
-                                                                             bool accumulate) {
+template <class In, int V, bool kAdd>
+__global__ __launch_bounds__(kSumThreads) void tlc_embedding_grad_sum_kernel(EmbArgs a,
+                                                                             SumArgs s) {
   __shared__ float lds[kSumWaves][64 * V];
   __shared__ uint32_t head[kSumWaves];
   const uint32_t lane = threadIdx.x & 63u, wid = uniform32(threadIdx.x >> 6);
@@ -444,12 +466,12 @@ __global__ __launch_bounds__(kSumThreads) void tlc_embedding_grad_sum_kernel(Emb
   const Columns<V> col(a.dim, s.packs, s.slabs, slab);
   const uint32_t c0 = umin32((block * kSumWaves + wid) * s.per_wave, a.count);
   const uint32_t c1 = umin32(c0 + s.per_wave, a.count);
-  WaveRuns<In, V> runs;
-  runs.run(a, s.keys, s.pos, a.count, c0, c1, col, &lds[wid][lane * V], accumulate);
+  WaveRuns<In, V, kAdd> runs;
+  runs.run(a, s.keys, s.pos, a.count, c0, c1, col, &lds[wid][lane * V]);
   if (lane == 0) head[wid] = runs.head;
   __syncthreads();
   float* parts = s.parts + (uint64_t)block * 2 * a.dim + col.k;
-  if (runs.tail && !runs.template finish<kSumWaves>(a, lds, head, wid, col, accumulate) && col.in)
+  if (runs.tail && !runs.template finish<kSumWaves>(a, lds, head, wid, col) && col.in)
     put_floats<V>(parts + a.dim, runs.sum.v);
   if (wid == 0 && head[0]) {
     Sum<V> sum = {};
@@ -464,9 +486,9 @@ __global__ __launch_bounds__(kSumThreads) void tlc_embedding_grad_sum_kernel(Emb
 // Runs that go on past a block: the block where one begins adds its tail and
 // the heads of the blocks after it, in their order.  Also leaves the
 // touched rows' marks as they were before the call.
-template <int V>
+template <int V, bool kAdd>
 __global__ __launch_bounds__(kJoinThreads) void tlc_embedding_grad_join_kernel(
-    EmbArgs a, SumArgs s, bool accumulate, uint8_t* __restrict__ touched) {
+    EmbArgs a, SumArgs s, uint8_t* __restrict__ touched) {
   constexpr int kParts = 8;  // partial rows in flight
   constexpr uint32_t kWavesJ = kJoinThreads / 64;
   __shared__ float lds[kWavesJ][64 * V];
@@ -517,7 +539,7 @@ __global__ __launch_bounds__(kJoinThreads) void tlc_embedding_grad_join_kernel(
     __syncthreads();
     if (wid == 0 && col.in) {
       for (uint32_t w = 1; w < kWavesJ && w * per < n; ++w) sum.add(&lds[w][lane * V]);
-      put_row<V>(a, row, col.k, sum.v, accumulate);
+      put_row<V, kAdd>(a, row, col.k, sum.v);
     }
     __syncthreads();
   }
@@ -560,14 +582,14 @@ int sort_tokens(const EmbArgs& a, const GradWork& w, uint32_t passes, FillArgs f
   return passes & 1;
 }
 
-template <class In, int V>
-void launch_grad(const EmbArgs& a, bool accumulate, const GradWork& w, hipStream_t st) {
+template <class In, int V, bool kAdd>
+void launch_grad(const EmbArgs& a, const GradWork& w, hipStream_t st) {
   // passes over the bits of 0 .. rows
   const uint32_t bits = 32 - (uint32_t)__builtin_clz(a.rows);
   const uint32_t passes = (bits + kDigitBits - 1) / kDigitBits;
   const bool small = a.count <= kSmallTokens;
   FillArgs f = {};
-  if (!accumulate) {
+  if (!kAdd) {
     const uint32_t packs = a.dim >= 4 ? (a.dim + 3) / 4 : a.dim;
     f.out = static_cast<float*>(a.out);
     f.out_stride = a.out_stride;
@@ -590,11 +612,11 @@ void launch_grad(const EmbArgs& a, bool accumulate, const GradWork& w, hipStream
     s.blocks = (a.count + s.per_wave - 1) / s.per_wave;
     const uint32_t grid = s.blocks * s.slabs + f.blocks;
     if (a.count <= kSmallThreads)
-      launch_k(tlc_embedding_grad_small_kernel<In, V, 1>, grid, kSmallThreads, st, a, s,
-               accumulate, passes, f);
+      launch_k(tlc_embedding_grad_small_kernel<In, V, kAdd, 1>, grid, kSmallThreads, st, a, s,
+               passes, f);
     else
-      launch_k(tlc_embedding_grad_small_kernel<In, V, 4>, grid, kSmallThreads, st, a, s,
-               accumulate, passes, f);
+      launch_k(tlc_embedding_grad_small_kernel<In, V, kAdd, 4>, grid, kSmallThreads, st, a, s,
+               passes, f);
     return;
   }
   const int at = a.count > kWideTileTokens ? sort_tokens<16>(a, w, passes, f, st)
@@ -603,15 +625,14 @@ void launch_grad(const EmbArgs& a, bool accumulate, const GradWork& w, hipStream
   s.pos = w.pos[at];
   s.per_wave = sum_per_wave(a.count, s.slabs);
   s.blocks = (a.count + s.per_wave * kSumWaves - 1) / (s.per_wave * kSumWaves);
-  launch_k(tlc_embedding_grad_sum_kernel<In, V>, s.blocks * s.slabs, kSumThreads, st, a, s,
-           accumulate);
-  uint8_t* touched = accumulate ? nullptr : w.touched;
+  launch_k(tlc_embedding_grad_sum_kernel<In, V, kAdd>, s.blocks * s.slabs, kSumThreads, st, a, s);
+  uint8_t* touched = kAdd ? nullptr : w.touched;
   if (a.dim >= 4)
-    launch_k(tlc_embedding_grad_join_kernel<4>, dim3(s.blocks, std::min((a.dim + 255) / 256, 8u)),
-             kJoinThreads, st, a, s, accumulate, touched);
+    launch_k(tlc_embedding_grad_join_kernel<4, kAdd>,
+             dim3(s.blocks, std::min((a.dim + 255) / 256, 8u)), kJoinThreads, st, a, s, touched);
   else
-    launch_k(tlc_embedding_grad_join_kernel<1>, dim3(s.blocks, 1), kJoinThreads, st, a, s,
-             accumulate, touched);
+    launch_k(tlc_embedding_grad_join_kernel<1, kAdd>, dim3(s.blocks, 1), kJoinThreads, st, a, s,
+             touched);
 }
 
 }  // namespace
@@ -620,10 +641,11 @@ hipError_t launch_embedding_grad(const EmbArgs& a, int grad_type, bool accumulat
                                  const GradWork& w, hipStream_t st) {
   with_type(grad_type, [&](auto in) {
     using In = decltype(in);
-    if (a.dim >= 16 / sizeof(In))
-      launch_grad<In, 16 / sizeof(In)>(a, accumulate, w, st);
+    constexpr int V = 16 / sizeof(In);
+    if (a.dim >= V)
+      accumulate ? launch_grad<In, V, true>(a, w, st) : launch_grad<In, V, false>(a, w, st);
     else
-      launch_grad<In, 1>(a, accumulate, w, st);
+      accumulate ? launch_grad<In, 1, true>(a, w, st) : launch_grad<In, 1, false>(a, w, st);
   });
   return hipGetLastError();
 }
