@@ -79,13 +79,15 @@ __device__ __forceinline__ uint64_t same_digit(uint32_t d, bool in) {
 }
 
 // A wave's rank of its keys among those of equal digit, 64 neighbouring keys at
-// a time; n: the wave's counts, zero before, its keys per digit after.
+// a time (`items` keys in all); n: the wave's counts, zero before, its keys per
+// digit after.
 template <int kItems>
 __device__ __forceinline__ void rank_keys(const uint32_t (&key)[kItems], uint32_t items,
                                           uint32_t shift, uint16_t* n, uint32_t (&rank)[kItems]) {
   const uint64_t below = lanes_below();
 #pragma unroll
   for (int i = 0; i < kItems; ++i) {
+    if (i * 64u >= items) break;
     const bool in = i * 64 + (threadIdx.x & 63u) < items;
     const uint32_t d = (key[i] >> shift) & kDigitMask;
     const uint64_t same = same_digit(d, in);
@@ -153,7 +155,7 @@ __device__ __forceinline__ void sort_block(uint32_t (&key)[kItems], uint32_t pas
 
 // The counts of a pass's digits in every tile; the first pass's also makes the
 // keys, and marks the rows that any token touches (touched NULL: not wanted).
-// Blocks from `tiles` on fill rows.
+// Clears the tables of the s.clear passes after it.  Blocks from `tiles` on fill rows.
 template <int kItems>
 __global__ __launch_bounds__(kSortThreads) void tlc_token_count_kernel(
     EmbArgs a, SortArgs s, uint32_t* __restrict__ keys, uint8_t* __restrict__ touched,
@@ -181,17 +183,24 @@ __global__ __launch_bounds__(kSortThreads) void tlc_token_count_kernel(
     atomicAdd(&n[(key >> s.shift) & kDigitMask], 1u);
   }
   __syncthreads();
-  if (threadIdx.x < kDigits) s.counts[blockIdx.x * kDigits + threadIdx.x] = n[threadIdx.x];
+  if (threadIdx.x < kDigits) {
+    const uint32_t at = blockIdx.x * kDigits + threadIdx.x;
+    s.counts[at] = n[threadIdx.x];
+    for (uint32_t p = 1; p <= s.clear; ++p) s.counts[p * s.tiles * kDigits + at] = 0u;
+  }
 }
 
 // One pass over tiles: a tile's keys go where the counts of all tiles send them,
-// those of equal digits in their order.
-template <int kItems>
+// those of equal digits in their order.  kNext: also counts the next pass's
+// digits in the tiles that the keys go to (at most kNextTiles), first in LDS:
+// added in memory key by key the counts of common rows took 20 us.
+template <int kItems, bool kNext>
 __global__ __launch_bounds__(kSortThreads) void tlc_token_sort_kernel(SortArgs s, FillArgs f) {
   constexpr int kW = kSortThreads / 64;
   __shared__ uint16_t wave_n[kW][kDigits];
   __shared__ uint32_t base[kDigits];
   __shared__ uint32_t scan_lds[kW];
+  __shared__ uint32_t next[kNext ? kNextTiles * kDigits : 1];
   if (blockIdx.x >= s.tiles) {
     const uint32_t b = f.block0 + blockIdx.x - s.tiles;
     fill_rows<kSortThreads>(f, b, f.touched + (uint64_t)b * f.block_rows);
@@ -210,6 +219,8 @@ __global__ __launch_bounds__(kSortThreads) void tlc_token_sort_kernel(SortArgs s
   }
 #pragma unroll
   for (int w = 0; w < kW; ++w) wave_n[w][threadIdx.x] = 0;
+  if (kNext)
+    for (uint32_t i = threadIdx.x; i < s.tiles * kDigits; i += kSortThreads) next[i] = 0u;
   // the digit's keys in the tiles before this one, and in all
   uint32_t before = 0, total = 0;
 #pragma unroll 16
@@ -231,6 +242,15 @@ __global__ __launch_bounds__(kSortThreads) void tlc_token_sort_kernel(SortArgs s
     const uint32_t to = base[d] + wave_n[wid][d] + rank[i];
     s.keys_out[to] = key[i];
     s.pos_out[to] = pos[i];
+    if (kNext)
+      atomicAdd(&next[to / (kSortThreads * kItems) * kDigits +
+                      ((key[i] >> (s.shift + kDigitBits)) & kDigitMask)],
+                1u);
+  }
+  if (kNext) {
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < s.tiles * kDigits; i += kSortThreads)
+      if (next[i]) atomicAdd(&s.next[i], next[i]);
   }
 }
 
@@ -462,7 +482,13 @@ __global__ __launch_bounds__(kSumThreads) void tlc_embedding_grad_sum_kernel(Emb
   __shared__ float lds[kSumWaves][64 * V];
   __shared__ uint32_t head[kSumWaves];
   const uint32_t lane = threadIdx.x & 63u, wid = uniform32(threadIdx.x >> 6);
-  const uint32_t block = blockIdx.x / s.slabs, slab = blockIdx.x % s.slabs;
+  // The slabs of the same tokens go to one XCD (blocks are dealt to the eight in
+  // turn), one after the other: their rows' pieces are read, and written, close
+  // together in one L2 (slab by slab over all tokens 394 instead of 342 us for
+  // 131072 tokens of 2048 bf16 values).
+  const uint32_t j = blockIdx.x / kXcds;
+  const uint32_t slab = j % s.slabs, block = j / s.slabs * kXcds + blockIdx.x % kXcds;
+  if (block >= s.blocks) return;
   const Columns<V> col(a.dim, s.packs, s.slabs, slab);
   const uint32_t c0 = umin32((block * kSumWaves + wid) * s.per_wave, a.count);
   const uint32_t c1 = umin32(c0 + s.per_wave, a.count);
@@ -563,21 +589,30 @@ int sort_tokens(const EmbArgs& a, const GradWork& w, uint32_t passes, FillArgs f
   SortArgs s = {};
   s.count = a.count;
   s.tiles = (a.count + kTile - 1) / kTile;
-  s.counts = w.counts;
   uint8_t* touched = f.blocks ? w.touched : nullptr;
+  const bool next = s.tiles <= kNextTiles;  // a pass counts for the one after it
   uint32_t left = f.blocks;
+  uint32_t launches = next ? passes : 2 * passes - 1;  // that take a share of the fill
   for (uint32_t p = 0; p < passes; ++p) {
     s.keys_in = w.keys[p & 1];
     s.pos_in = p ? w.pos[p & 1] : nullptr;
     s.keys_out = w.keys[(p + 1) & 1];
     s.pos_out = w.pos[(p + 1) & 1];
+    s.counts = w.counts + (next ? p * s.tiles * kDigits : 0);
+    s.next = next && p + 1 < passes ? s.counts + s.tiles * kDigits : nullptr;
+    s.clear = next && p == 0 ? passes - 1 : 0;
     s.shift = p * kDigitBits;
-    // no fill beside the first count, which makes the marks
-    uint32_t fill = p ? take_fill(&f, &left, 2 * (passes - p)) : 0;
-    launch_k(tlc_token_count_kernel<kItems>, s.tiles + fill, kSortThreads, st, a, s, w.keys[0],
-             touched, f);
-    fill = take_fill(&f, &left, 2 * (passes - p) - 1);
-    launch_k(tlc_token_sort_kernel<kItems>, s.tiles + fill, kSortThreads, st, s, f);
+    if (p == 0 || !next) {
+      // no fill beside the first count, which makes the marks
+      const uint32_t fill = p ? take_fill(&f, &left, launches--) : 0;
+      launch_k(tlc_token_count_kernel<kItems>, s.tiles + fill, kSortThreads, st, a, s, w.keys[0],
+               touched, f);
+    }
+    const uint32_t fill = take_fill(&f, &left, launches--);
+    if (s.next)
+      launch_k(tlc_token_sort_kernel<kItems, true>, s.tiles + fill, kSortThreads, st, s, f);
+    else
+      launch_k(tlc_token_sort_kernel<kItems, false>, s.tiles + fill, kSortThreads, st, s, f);
   }
   return passes & 1;
 }
@@ -615,7 +650,7 @@ void launch_grad(const EmbArgs& a, const GradWork& w, hipStream_t st) {
       launch_k(tlc_embedding_grad_small_kernel<In, V, kAdd, 1>, grid, kSmallThreads, st, a, s,
                passes, f);
     else
-      launch_k(tlc_embedding_grad_small_kernel<In, V, kAdd, 4>, grid, kSmallThreads, st, a, s,
+      launch_k(tlc_embedding_grad_small_kernel<In, V, kAdd, 2>, grid, kSmallThreads, st, a, s,
                passes, f);
     return;
   }
@@ -625,7 +660,8 @@ void launch_grad(const EmbArgs& a, const GradWork& w, hipStream_t st) {
   s.pos = w.pos[at];
   s.per_wave = sum_per_wave(a.count, s.slabs);
   s.blocks = (a.count + s.per_wave * kSumWaves - 1) / (s.per_wave * kSumWaves);
-  launch_k(tlc_embedding_grad_sum_kernel<In, V, kAdd>, s.blocks * s.slabs, kSumThreads, st, a, s);
+  launch_k(tlc_embedding_grad_sum_kernel<In, V, kAdd>,
+           (s.blocks + kXcds - 1) / kXcds * kXcds * s.slabs, kSumThreads, st, a, s);
   uint8_t* touched = kAdd ? nullptr : w.touched;
   if (a.dim >= 4)
     launch_k(tlc_embedding_grad_join_kernel<4, kAdd>,

@@ -200,7 +200,8 @@ TLC_API int tlc_train_create(tlc_train** out, size_t max_tokens, size_t max_rows
     off = round_up(off + max_tokens * sizeof(uint32_t), 256);
   }
   const size_t off_counts = off;
-  off = round_up(off + ceil_div(max_tokens, kSortTile) * kDigits * sizeof(uint32_t), 256);
+  off = round_up(off + kSortPasses * ceil_div(max_tokens, kSortTile) * kDigits * sizeof(uint32_t),
+                 256);
   const size_t off_touched = off;
   off = round_up(off + max_rows, 256);
   const size_t off_parts = off;
