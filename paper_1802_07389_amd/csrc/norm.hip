@@ -1,4 +1,6 @@
 // norm.hip -- the global norm of a list of tensors, and their clipping.
+#include <type_traits>
+
 #include "device_common.hpp"
 #include "train_internal.h"
 #include "typed_io.hpp"
@@ -39,49 +41,107 @@ __device__ __forceinline__ Clip clip_of(double sumsq, float max_norm) {
   return c;
 }
 
-__device__ __forceinline__ void put_result(tlc_norm_result* r, double sumsq, Clip c) {
-  r->sumsq = sumsq;
+__device__ __forceinline__ void put_result(tlc_norm_result* r, Clip c) {
   r->norm = c.norm;
   r->coef = c.coef;
   r->status = c.finite ? TLC_OK : TLC_E_NONFINITE;
   r->reserved = 0u;
 }
 
-template <class T>
-__device__ __forceinline__ double piece_sumsq(const Piece& p) {
-  const T* x = static_cast<const T*>(p.x);
-  double v = 0.0;
-  for (uint32_t i = threadIdx.x; i < p.n; i += kNormThreads) {
-    const double d = (double)(float)x[i];
-    v += d * d;
-  }
-  return v;
+// Piece p of a list.
+__device__ __forceinline__ Piece piece_of(const ListArgs& list, uint32_t p) {
+  if (list.pieces) return list.pieces[p];
+  const uint32_t lane = threadIdx.x & 63u;
+  uint32_t t = 0;  // tensors whose first piece is at most p
+  for (uint32_t c = 0; c < list.count; c += 64)
+    t += (uint32_t)__popcll(__ballot(
+        c + lane < list.count && (list.tensors[c + lane].piece0_type & 0x3fffffffu) <= p));
+  const ListTensor& e = list.tensors[uniform32(t) - 1];
+  const uint64_t first = (uint64_t)(p - (e.piece0_type & 0x3fffffffu)) * list.len;
+  Piece r;
+  r.type = e.piece0_type >> 30;
+  const uint32_t size = r.type == TLC_F32 ? 4 : 2;
+  r.x = static_cast<const uint8_t*>(e.x) + first * size;
+  r.out = static_cast<uint8_t*>(e.out) + first * (list.own_type ? size : 4);
+  r.n = (uint32_t)umin64(list.len, e.n - first);
+  return r;
 }
 
-template <class T, class Out>
+constexpr uint32_t kUnits = 8;  // packs of a thread in flight
+
+template <class T, bool kStream>
+__device__ __forceinline__ double piece_sumsq(const Piece& p) {
+  constexpr int V = 16 / sizeof(T);
+  const T* x = static_cast<const T*>(p.x);
+  const uint32_t packs = p.n / V;
+  double v[4] = {0.0, 0.0, 0.0, 0.0};
+  for (uint32_t u0 = threadIdx.x; u0 < packs; u0 += kNormThreads * kUnits) {
+    Pack<T, V> r[kUnits];
+#pragma unroll
+    for (uint32_t i = 0; i < kUnits; ++i) {
+      const uint32_t u = u0 + i * kNormThreads;
+      r[i] = load_pack<T, V, kStream>(x + umin32(u, packs - 1) * V);
+      if (u >= packs) r[i] = {};
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kUnits; ++i)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const double d = (double)r[i].get(e);
+        v[e & 3] = __builtin_fma(d, d, v[e & 3]);
+      }
+  }
+  if (threadIdx.x < p.n - packs * V) {
+    const double d = (double)(float)x[packs * V + threadIdx.x];
+    v[0] = __builtin_fma(d, d, v[0]);
+  }
+  return (v[0] + v[1]) + (v[2] + v[3]);
+}
+
+template <class T, class Out, bool kStream>
 __device__ __forceinline__ void piece_scale(const Piece& p, float coef) {
+  constexpr int V = 16 / sizeof(T);
   const T* x = static_cast<const T*>(p.x);
   Out* out = static_cast<Out*>(p.out);
-  for (uint32_t i = threadIdx.x; i < p.n; i += kNormThreads) out[i] = round_to<Out>(coef * (float)x[i]);
+  const uint32_t packs = p.n / V;
+  for (uint32_t u0 = threadIdx.x; u0 < packs; u0 += kNormThreads * kUnits) {
+    Pack<T, V> r[kUnits];
+#pragma unroll
+    for (uint32_t i = 0; i < kUnits; ++i)
+      r[i] = load_pack<T, V, kStream>(x + umin32(u0 + i * kNormThreads, packs - 1) * V);
+#pragma unroll
+    for (uint32_t i = 0; i < kUnits; ++i) {
+      const uint32_t u = u0 + i * kNormThreads;
+      if (u >= packs) break;
+      Pack<Out, V> o;
+#pragma unroll
+      for (int e = 0; e < V; ++e) o.set(e, coef * r[i].get(e));
+      store_pack<Out, V, kStream>(out + u * V, o);
+    }
+  }
+  if (threadIdx.x < p.n - packs * V) {
+    const uint32_t i = packs * V + threadIdx.x;
+    out[i] = round_to<Out>(coef * (float)x[i]);
+  }
 }
 
 }  // namespace
 
-__global__ __launch_bounds__(kNormThreads) void tlc_sumsq_kernel(const Piece* __restrict__ pieces,
-                                                                 uint32_t n,
+template <bool kStream>
+__global__ __launch_bounds__(kNormThreads) void tlc_sumsq_kernel(ListArgs list,
                                                                  double* __restrict__ partials) {
   __shared__ double lds[kWaves];
-  const uint32_t p0 = (uint32_t)((uint64_t)blockIdx.x * n / gridDim.x);
-  const uint32_t p1 = (uint32_t)((uint64_t)(blockIdx.x + 1) * n / gridDim.x);
+  const uint32_t p0 = (uint32_t)((uint64_t)blockIdx.x * list.n / gridDim.x);
+  const uint32_t p1 = (uint32_t)((uint64_t)(blockIdx.x + 1) * list.n / gridDim.x);
   double v = 0.0;
   for (uint32_t i = p0; i < p1; ++i) {
-    const Piece p = pieces[i];
+    const Piece p = piece_of(list, i);
     if (p.type == TLC_F32)
-      v += piece_sumsq<float>(p);
+      v += piece_sumsq<float, kStream>(p);
     else if (p.type == TLC_BF16)
-      v += piece_sumsq<bf16_t>(p);
+      v += piece_sumsq<bf16_t, kStream>(p);
     else
-      v += piece_sumsq<f16_t>(p);
+      v += piece_sumsq<f16_t, kStream>(p);
   }
   v = block_sum(v, lds);
   if (threadIdx.x == 0) partials[blockIdx.x] = v;
@@ -91,42 +151,45 @@ __global__ __launch_bounds__(kNormThreads) void tlc_norm_finish_kernel(
     const double* __restrict__ partials, uint32_t np, tlc_norm_result* __restrict__ result) {
   __shared__ double lds[kWaves];
   const double sumsq = sum_partials(partials, np, lds);
-  if (threadIdx.x == 0) put_result(result, sumsq, clip_of(sumsq, INFINITY));
+  if (threadIdx.x != 0) return;
+  result->sumsq = sumsq;
+  put_result(result, clip_of(sumsq, INFINITY));
 }
 
+// Out: float, or void: the tensors' own types.
+template <class Out, bool kStream>
 __global__ __launch_bounds__(kNormThreads) void tlc_clip_kernel(
-    const Piece* __restrict__ pieces, uint32_t n, const double* __restrict__ partials, uint32_t np,
-    float max_norm, bool own_type, tlc_norm_result* __restrict__ result) {
+    ListArgs list, const double* __restrict__ partials, uint32_t np, float max_norm,
+    tlc_norm_result* __restrict__ result) {
+  constexpr bool kOwn = __is_same(Out, void);
   __shared__ double lds[kWaves];
-  // sumsq is read by every block; block 0 writes it back as it is
+  // sumsq is read by every block; the first one writes the rest
   const double sumsq = partials ? sum_partials(partials, np, lds) : result->sumsq;
   const Clip c = clip_of(sumsq, max_norm);
   if (blockIdx.x == 0 && threadIdx.x == 0) {
-    if (partials) {
-      put_result(result, sumsq, c);
-    } else {
-      result->norm = c.norm;
-      result->coef = c.coef;
-      result->status = c.finite ? TLC_OK : TLC_E_NONFINITE;
-      result->reserved = 0u;
-    }
+    if (partials) result->sumsq = sumsq;
+    put_result(result, c);
   }
-  if (!c.finite || (own_type && c.coef == 1.0f)) return;
-  const uint32_t p0 = (uint32_t)((uint64_t)blockIdx.x * n / gridDim.x);
-  const uint32_t p1 = (uint32_t)((uint64_t)(blockIdx.x + 1) * n / gridDim.x);
+  if (!c.finite || (kOwn && c.coef == 1.0f)) return;
+  const uint32_t p0 = (uint32_t)((uint64_t)blockIdx.x * list.n / gridDim.x);
+  const uint32_t p1 = (uint32_t)((uint64_t)(blockIdx.x + 1) * list.n / gridDim.x);
   for (uint32_t i = p0; i < p1; ++i) {
-    const Piece p = pieces[i];
+    Piece p = piece_of(list, i);
     if (p.type == TLC_F32)
-      piece_scale<float, float>(p, c.coef);
+      piece_scale<float, float, kStream>(p, c.coef);
     else if (p.type == TLC_BF16)
-      own_type ? piece_scale<bf16_t, bf16_t>(p, c.coef) : piece_scale<bf16_t, float>(p, c.coef);
+      piece_scale<bf16_t, std::conditional_t<kOwn, bf16_t, float>, kStream>(p, c.coef);
     else
-      own_type ? piece_scale<f16_t, f16_t>(p, c.coef) : piece_scale<f16_t, float>(p, c.coef);
+      piece_scale<f16_t, std::conditional_t<kOwn, f16_t, float>, kStream>(p, c.coef);
   }
 }
 
-hipError_t launch_sumsq(const Piece* pieces, uint32_t n, double* partials, hipStream_t st) {
-  if (n) launch_k(tlc_sumsq_kernel, norm_blocks(n), kNormThreads, st, pieces, n, partials);
+hipError_t launch_sumsq(const ListArgs& list, double* partials, hipStream_t st) {
+  if (list.n == 0) return hipSuccess;
+  if (list.stream)
+    launch_k(tlc_sumsq_kernel<true>, norm_blocks(list.n), kNormThreads, st, list, partials);
+  else
+    launch_k(tlc_sumsq_kernel<false>, norm_blocks(list.n), kNormThreads, st, list, partials);
   return hipGetLastError();
 }
 
@@ -136,10 +199,28 @@ hipError_t launch_norm_finish(const double* partials, uint32_t np, tlc_norm_resu
   return hipGetLastError();
 }
 
-hipError_t launch_clip(const Piece* pieces, uint32_t n, const double* partials, uint32_t np,
-                       float max_norm, bool own_type, tlc_norm_result* result, hipStream_t st) {
-  launch_k(tlc_clip_kernel, std::max(1u, norm_blocks(n)), kNormThreads, st, pieces, n, partials,
-           np, max_norm, own_type, result);
+namespace {
+
+template <class Out>
+void launch_clip_to(const ListArgs& list, const double* partials, uint32_t np, float max_norm,
+                    tlc_norm_result* result, hipStream_t st) {
+  const uint32_t grid = std::max(1u, norm_blocks(list.n));
+  if (list.stream)
+    launch_k(tlc_clip_kernel<Out, true>, grid, kNormThreads, st, list, partials, np, max_norm,
+             result);
+  else
+    launch_k(tlc_clip_kernel<Out, false>, grid, kNormThreads, st, list, partials, np, max_norm,
+             result);
+}
+
+}  // namespace
+
+hipError_t launch_clip(const ListArgs& list, const double* partials, uint32_t np, float max_norm,
+                       tlc_norm_result* result, hipStream_t st) {
+  if (list.own_type)
+    launch_clip_to<void>(list, partials, np, max_norm, result, st);
+  else
+    launch_clip_to<float>(list, partials, np, max_norm, result, st);
   return hipGetLastError();
 }
 

@@ -1,7 +1,6 @@
 // train_api.hip -- host side of the training-step operators of include/tlc.h:
 // argument checks, their context's workspace and the launches on its stream.
 #include <math.h>
-#include <string.h>
 
 #include <new>
 #include <vector>
@@ -38,19 +37,18 @@ struct tlc_train {
   bool broken = false;
   // device workspace (one allocation)
   void* ws = nullptr;
-  Piece* pieces = nullptr;
   double* partials = nullptr;
   GradWork grad = {};
   // pinned: the sticky index flag and the staging slots of the pieces
   uint32_t* bad = nullptr;
   uint32_t* bad_dev = nullptr;
   Piece* staging = nullptr;
+  Piece* staging_dev = nullptr;  // the same, as the device addresses it
   size_t slot_pieces = 0;
   hipEvent_t slot_done[kSlots] = {};
   bool slot_used[kSlots] = {};
   int slot_next = 0;
   // host tables, reserved at creation so that the calls do not allocate
-  std::vector<Piece> host_pieces;
   std::vector<Span> spans, spans_ok;
 };
 
@@ -84,11 +82,25 @@ int check_table(const char* fn, size_t rows, size_t dim, int ids_type, int value
   return TLC_OK;
 }
 
-// Checks a list of tensors and cuts it into pieces (c->host_pieces).  clip:
-// the tensors are scaled into outs, or in place (outs NULL).
+// A pinned slot, free once the kernels of its last call have run.
+int take_slot(tlc_train* c, int* slot) {
+  *slot = c->slot_next;
+  c->slot_next = (*slot + 1) % kSlots;
+  if (c->slot_used[*slot]) {
+    const hipError_t e = hipEventSynchronize(c->slot_done[*slot]);
+    if (e != hipSuccess) return hip_fail(e, "hipEventSynchronize(staging)");
+    c->slot_used[*slot] = false;
+  }
+  return TLC_OK;
+}
+
+// Checks a list of tensors and cuts it into pieces: into l's table, or into a
+// pinned slot (*slot, to be held after the kernels that read it; else -1).
+// clip: the tensors are scaled into outs, or in place (outs NULL).
 int cut_list(tlc_train* c, const char* fn, size_t count, const void* const* tensors,
              const int* types, const size_t* ns, tlc_norm_result* result, bool clip,
-             float* const* outs) {
+             float* const* outs, ListArgs* l, int* slot) {
+  *slot = -1;
   int st = check_usable(c, fn);
   if (st) return st;
   if (!result) return fail(TLC_E_INVALID, "%s: NULL result", fn);
@@ -96,7 +108,7 @@ int cut_list(tlc_train* c, const char* fn, size_t count, const void* const* tens
   if (count > c->max_tensors)
     return fail(TLC_E_INVALID, "%s: %zu tensors exceed the context's %zu", fn, count,
                 c->max_tensors);
-  size_t total = 0;
+  size_t total = 0, total_bytes = 0;
   c->spans.clear();
   add_span(c->spans, result, sizeof(*result), true);
   for (size_t i = 0; i < count; ++i) {
@@ -109,6 +121,7 @@ int cut_list(tlc_train* c, const char* fn, size_t count, const void* const* tens
       return fail(TLC_E_INVALID, "%s: tensor %zu: NULL pointer", fn, i);
     total += ns[i];
     const size_t bytes = ns[i] * type_bytes(types[i]);
+    total_bytes += bytes;
     const bool in_place =
         clip && (!outs || ((const void*)outs[i] == tensors[i] && types[i] == TLC_F32));
     add_span(c->spans, tensors[i], bytes, in_place);
@@ -118,42 +131,44 @@ int cut_list(tlc_train* c, const char* fn, size_t count, const void* const* tens
     return fail(TLC_E_INVALID, "%s: %zu values exceed %zu", fn, total, kMaxListValues);
   if (spans_conflict_cached(c->spans, c->spans_ok))
     return fail(TLC_E_INVALID, "%s: a written buffer overlaps another one", fn);
-  const uint64_t len =
-      std::max<uint64_t>(1, ceil_div(ceil_div(total, kNormBlocks), kPieceValues)) * kPieceValues;
-  c->host_pieces.clear();
+  l->own_type = clip && !outs;
+  l->stream = total_bytes > kCacheBytes;
+  l->len = (uint32_t)(std::max<size_t>(1, ceil_div(ceil_div(total, kNormBlocks), kPieceValues)) *
+                      kPieceValues);
+  if (count <= kArgTensors) {
+    for (size_t i = 0; i < count; ++i) {
+      if (ns[i] == 0) continue;
+      ListTensor& e = l->tensors[l->count++];
+      e.x = tensors[i];
+      e.out = outs ? (void*)outs[i] : (void*)tensors[i];
+      e.n = (uint32_t)ns[i];
+      e.piece0_type = l->n | (uint32_t)types[i] << 30;
+      l->n += (uint32_t)ceil_div(ns[i], l->len);
+    }
+    return TLC_OK;
+  }
+  st = take_slot(c, slot);
+  if (st) return st;
+  Piece* host = c->staging + (size_t)*slot * c->slot_pieces;
+  l->pieces = c->staging_dev + (size_t)*slot * c->slot_pieces;
   for (size_t i = 0; i < count; ++i) {
     const size_t size = type_bytes(types[i]);
-    for (size_t k = 0; k < ns[i]; k += len) {
-      Piece p;
+    for (size_t k = 0; k < ns[i]; k += l->len) {
+      Piece& p = host[l->n++];
       p.x = (const uint8_t*)tensors[i] + k * size;
-      p.out = !clip ? nullptr
-                    : (outs ? (void*)(outs[i] + k) : (void*)((uint8_t*)tensors[i] + k * size));
-      p.n = (uint32_t)std::min<size_t>(len, ns[i] - k);
+      p.out = outs ? (void*)(outs[i] + k) : (void*)p.x;
+      p.n = (uint32_t)std::min<size_t>(l->len, ns[i] - k);
       p.type = (uint32_t)types[i];
-      c->host_pieces.push_back(p);
     }
   }
   return TLC_OK;
 }
 
-// Copies the pieces to the device through a pinned slot; a slot is filled
-// again only after its previous copy has run.
-int upload_pieces(tlc_train* c) {
-  const size_t n = c->host_pieces.size();
-  if (n == 0) return TLC_OK;
-  const int slot = c->slot_next;
-  c->slot_next = (slot + 1) % kSlots;
-  if (c->slot_used[slot]) {
-    const hipError_t e = hipEventSynchronize(c->slot_done[slot]);
-    if (e != hipSuccess) return hip_fail(e, "hipEventSynchronize(staging)");
-    c->slot_used[slot] = false;
-  }
-  Piece* host = c->staging + (size_t)slot * c->slot_pieces;
-  memcpy(host, c->host_pieces.data(), n * sizeof(Piece));
-  hipError_t e =
-      hipMemcpyAsync(c->pieces, host, n * sizeof(Piece), hipMemcpyHostToDevice, c->stream);
-  if (e == hipSuccess) e = hipEventRecord(c->slot_done[slot], c->stream);
-  if (e != hipSuccess) return launched(c, e, "descriptor upload");
+// The staging slot is free again once the kernels queued so far have run.
+int hold_slot(tlc_train* c, int slot) {
+  if (slot < 0) return TLC_OK;
+  const hipError_t e = hipEventRecord(c->slot_done[slot], c->stream);
+  if (e != hipSuccess) return launched(c, e, "hipEventRecord(staging)");
   c->slot_used[slot] = true;
   return TLC_OK;
 }
@@ -188,12 +203,10 @@ TLC_API int tlc_train_create(tlc_train** out, size_t max_tokens, size_t max_rows
     delete c;
     return hip_fail(e, "hipGetDevice");
   }
-  c->slot_pieces = max_tensors ? kNormBlocks + max_tensors : 0;
-  // layout: pieces | partial sums | sorted tokens, twice | counts of the sort |
+  c->slot_pieces = max_tensors > kArgTensors ? kNormBlocks + max_tensors : 0;
+  // layout: partial sums | sorted tokens, twice | counts of the sort |
   //         touched rows | partial rows
-  size_t off = round_up(c->slot_pieces * sizeof(Piece), 256);
-  const size_t off_partials = off;
-  off = round_up(off + kNormBlocks * sizeof(double), 256);
+  size_t off = round_up(kNormBlocks * sizeof(double), 256);
   size_t off_sort[4];
   for (size_t& o : off_sort) {
     o = off;
@@ -215,6 +228,8 @@ TLC_API int tlc_train_create(tlc_train** out, size_t max_tokens, size_t max_rows
   if (e == hipSuccess && c->slot_pieces)
     e = hipHostMalloc((void**)&c->staging, kSlots * c->slot_pieces * sizeof(Piece),
                       hipHostMallocDefault);
+  if (e == hipSuccess && c->staging)
+    e = hipHostGetDevicePointer((void**)&c->staging_dev, c->staging, 0);
   for (int i = 0; i < kSlots && e == hipSuccess; ++i)
     e = hipEventCreateWithFlags(&c->slot_done[i], hipEventDisableTiming);
   if (e != hipSuccess) {
@@ -223,8 +238,7 @@ TLC_API int tlc_train_create(tlc_train** out, size_t max_tokens, size_t max_rows
   }
   *c->bad = 0u;
   uint8_t* base = (uint8_t*)c->ws;
-  c->pieces = (Piece*)base;
-  c->partials = (double*)(base + off_partials);
+  c->partials = (double*)base;
   for (int i = 0; i < 2; ++i) {
     c->grad.keys[i] = (uint32_t*)(base + off_sort[i]);
     c->grad.pos[i] = (uint32_t*)(base + off_sort[2 + i]);
@@ -233,7 +247,6 @@ TLC_API int tlc_train_create(tlc_train** out, size_t max_tokens, size_t max_rows
   c->grad.touched = base + off_touched;
   c->grad.parts = (float*)(base + off_parts);
   try {
-    c->host_pieces.reserve(c->slot_pieces);
     c->spans.reserve(2 * max_tensors + 1);
     c->spans_ok.reserve(2 * max_tensors + 1);
   } catch (...) {
@@ -360,52 +373,50 @@ TLC_API int tlc_embedding_grad(tlc_train* c, const void* grad, int grad_type, si
 TLC_API int tlc_grad_norm(tlc_train* c, size_t count, const void* const* tensors,
                           const int* types, const size_t* ns, tlc_norm_result* result) {
   const char* fn = "tlc_grad_norm";
-  int st = cut_list(c, fn, count, tensors, types, ns, result, false, nullptr);
+  ListArgs l = {};
+  int slot = -1;
+  int st = cut_list(c, fn, count, tensors, types, ns, result, false, nullptr, &l, &slot);
   if (st) return st;
   DeviceScope dev(c->device);
   st = dev.status();
   if (st) return st;
-  st = upload_pieces(c);
-  if (st) return st;
-  const uint32_t n = (uint32_t)c->host_pieces.size();
-  st = launched(c, launch_sumsq(c->pieces, n, c->partials, c->stream), fn);
-  if (st) return st;
-  return launched(c, launch_norm_finish(c->partials, norm_blocks(n), result, c->stream), fn);
+  st = launched(c, launch_sumsq(l, c->partials, c->stream), fn);
+  if (!st)
+    st = launched(c, launch_norm_finish(c->partials, norm_blocks(l.n), result, c->stream), fn);
+  return st ? st : hold_slot(c, slot);
 }
 
 TLC_API int tlc_clip(tlc_train* c, size_t count, const void* const* tensors, const int* types,
                      const size_t* ns, float max_norm, tlc_norm_result* result,
                      float* const* outs) {
   const char* fn = "tlc_clip";
+  ListArgs l = {};
+  int slot = -1;
   int st = check_clip(fn, max_norm);
-  if (!st) st = cut_list(c, fn, count, tensors, types, ns, result, true, outs);
+  if (!st) st = cut_list(c, fn, count, tensors, types, ns, result, true, outs, &l, &slot);
   if (st) return st;
   DeviceScope dev(c->device);
   st = dev.status();
   if (st) return st;
-  st = upload_pieces(c);
-  if (st) return st;
-  const uint32_t n = (uint32_t)c->host_pieces.size();
-  return launched(c, launch_clip(c->pieces, n, nullptr, 0, max_norm, !outs, result, c->stream),
-                  fn);
+  st = launched(c, launch_clip(l, nullptr, 0, max_norm, result, c->stream), fn);
+  return st ? st : hold_slot(c, slot);
 }
 
 TLC_API int tlc_clip_grad_norm(tlc_train* c, size_t count, const void* const* tensors,
                                const int* types, const size_t* ns, float max_norm,
                                tlc_norm_result* result, float* const* outs) {
   const char* fn = "tlc_clip_grad_norm";
+  ListArgs l = {};
+  int slot = -1;
   int st = check_clip(fn, max_norm);
-  if (!st) st = cut_list(c, fn, count, tensors, types, ns, result, true, outs);
+  if (!st) st = cut_list(c, fn, count, tensors, types, ns, result, true, outs, &l, &slot);
   if (st) return st;
   DeviceScope dev(c->device);
   st = dev.status();
   if (st) return st;
-  st = upload_pieces(c);
-  if (st) return st;
-  const uint32_t n = (uint32_t)c->host_pieces.size();
-  st = launched(c, launch_sumsq(c->pieces, n, c->partials, c->stream), fn);
-  if (st) return st;
-  return launched(c, launch_clip(c->pieces, n, c->partials, norm_blocks(n), max_norm, !outs,
-                                 result, c->stream),
+  st = launched(c, launch_sumsq(l, c->partials, c->stream), fn);
+  if (!st)
+    st = launched(c, launch_clip(l, c->partials, norm_blocks(l.n), max_norm, result, c->stream),
                   fn);
+  return st ? st : hold_slot(c, slot);
 }

@@ -102,20 +102,39 @@ struct Piece {
 };
 static_assert(sizeof(Piece) == 24, "Piece is 24 bytes");
 constexpr uint32_t kNormThreads = 256;
-constexpr uint32_t kNormBlocks = 2048;    // eight blocks on every CU
-constexpr uint64_t kPieceValues = 4096;   // pieces are multiples of this
+constexpr uint32_t kNormBlocks = 2048;   // eight blocks on every CU
+constexpr uint32_t kPieceValues = 4096;  // pieces are multiples of this
+
+// Up to kArgTensors tensors go to the kernels with their arguments, and a block
+// finds its pieces there; of more, the pieces are read in pinned host memory.
+constexpr uint32_t kArgTensors = 128;
+struct ListTensor {
+  const void* x;
+  void* out;
+  uint32_t n;
+  uint32_t piece0_type;  // its first piece, type in the top two bits
+};
+struct ListArgs {
+  const Piece* pieces;   // pinned, or NULL: tensors
+  uint32_t count, n;     // tensors, pieces
+  uint32_t len;          // values of a piece
+  bool own_type;         // clipping: out is of x's type (else fp32)
+  bool stream;           // the values don't fit the last-level cache
+  ListTensor tensors[kArgTensors];
+};
+static_assert(sizeof(ListArgs) <= 3328, "kernel arguments end at 4096 bytes");
 
 // The partial sums of the blocks (one double each) over `pieces` pieces.
 inline uint32_t norm_blocks(uint32_t pieces) {
   return pieces < kNormBlocks ? pieces : kNormBlocks;
 }
-hipError_t launch_sumsq(const Piece* pieces, uint32_t n, double* partials, hipStream_t st);
+hipError_t launch_sumsq(const ListArgs& list, double* partials, hipStream_t st);
 // Their sum into the result.
 hipError_t launch_norm_finish(const double* partials, uint32_t np, tlc_norm_result* result,
                               hipStream_t st);
 // The clipped tensors, from the partial sums or (partials NULL) from
-// result->sumsq.  own_type: in place in the pieces' own types.
-hipError_t launch_clip(const Piece* pieces, uint32_t n, const double* partials, uint32_t np,
-                       float max_norm, bool own_type, tlc_norm_result* result, hipStream_t st);
+// result->sumsq.
+hipError_t launch_clip(const ListArgs& list, const double* partials, uint32_t np, float max_norm,
+                       tlc_norm_result* result, hipStream_t st);
 
 }  // namespace tlc
