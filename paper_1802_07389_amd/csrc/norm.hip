@@ -49,8 +49,10 @@ __device__ __forceinline__ void put_result(tlc_norm_result* r, Clip c) {
 }
 
 // Piece p of a list.
-__device__ __forceinline__ Piece piece_of(const ListArgs& list, uint32_t p) {
-  if (list.pieces) return list.pieces[p];
+__device__ __forceinline__ Piece piece_of(const PinnedList& list, uint32_t p) {
+  return list.pieces[p];
+}
+__device__ __forceinline__ Piece piece_of(const ArgList& list, uint32_t p) {
   const uint32_t lane = threadIdx.x & 63u;
   uint32_t t = 0;  // tensors whose first piece is at most p
   for (uint32_t c = 0; c < list.count; c += 64)
@@ -127,8 +129,8 @@ __device__ __forceinline__ void piece_scale(const Piece& p, float coef) {
 
 }  // namespace
 
-template <bool kStream>
-__global__ __launch_bounds__(kNormThreads) void tlc_sumsq_kernel(ListArgs list,
+template <class List, bool kStream>
+__global__ __launch_bounds__(kNormThreads) void tlc_sumsq_kernel(List list,
                                                                  double* __restrict__ partials) {
   __shared__ double lds[kWaves];
   const uint32_t p0 = (uint32_t)((uint64_t)blockIdx.x * list.n / gridDim.x);
@@ -157,9 +159,9 @@ __global__ __launch_bounds__(kNormThreads) void tlc_norm_finish_kernel(
 }
 
 // Out: float, or void: the tensors' own types.
-template <class Out, bool kStream>
+template <class List, class Out, bool kStream>
 __global__ __launch_bounds__(kNormThreads) void tlc_clip_kernel(
-    ListArgs list, const double* __restrict__ partials, uint32_t np, float max_norm,
+    List list, const double* __restrict__ partials, uint32_t np, float max_norm,
     tlc_norm_result* __restrict__ result) {
   constexpr bool kOwn = __is_same(Out, void);
   __shared__ double lds[kWaves];
@@ -184,12 +186,13 @@ __global__ __launch_bounds__(kNormThreads) void tlc_clip_kernel(
   }
 }
 
-hipError_t launch_sumsq(const ListArgs& list, double* partials, hipStream_t st) {
+template <class List>
+hipError_t launch_sumsq(const List& list, double* partials, hipStream_t st) {
   if (list.n == 0) return hipSuccess;
   if (list.stream)
-    launch_k(tlc_sumsq_kernel<true>, norm_blocks(list.n), kNormThreads, st, list, partials);
+    launch_k(tlc_sumsq_kernel<List, true>, norm_blocks(list.n), kNormThreads, st, list, partials);
   else
-    launch_k(tlc_sumsq_kernel<false>, norm_blocks(list.n), kNormThreads, st, list, partials);
+    launch_k(tlc_sumsq_kernel<List, false>, norm_blocks(list.n), kNormThreads, st, list, partials);
   return hipGetLastError();
 }
 
@@ -201,21 +204,22 @@ hipError_t launch_norm_finish(const double* partials, uint32_t np, tlc_norm_resu
 
 namespace {
 
-template <class Out>
-void launch_clip_to(const ListArgs& list, const double* partials, uint32_t np, float max_norm,
+template <class Out, class List>
+void launch_clip_to(const List& list, const double* partials, uint32_t np, float max_norm,
                     tlc_norm_result* result, hipStream_t st) {
   const uint32_t grid = std::max(1u, norm_blocks(list.n));
   if (list.stream)
-    launch_k(tlc_clip_kernel<Out, true>, grid, kNormThreads, st, list, partials, np, max_norm,
+    launch_k(tlc_clip_kernel<List, Out, true>, grid, kNormThreads, st, list, partials, np, max_norm,
              result);
   else
-    launch_k(tlc_clip_kernel<Out, false>, grid, kNormThreads, st, list, partials, np, max_norm,
+    launch_k(tlc_clip_kernel<List, Out, false>, grid, kNormThreads, st, list, partials, np, max_norm,
              result);
 }
 
 }  // namespace
 
-hipError_t launch_clip(const ListArgs& list, const double* partials, uint32_t np, float max_norm,
+template <class List>
+hipError_t launch_clip(const List& list, const double* partials, uint32_t np, float max_norm,
                        tlc_norm_result* result, hipStream_t st) {
   if (list.own_type)
     launch_clip_to<void>(list, partials, np, max_norm, result, st);
@@ -223,5 +227,12 @@ hipError_t launch_clip(const ListArgs& list, const double* partials, uint32_t np
     launch_clip_to<float>(list, partials, np, max_norm, result, st);
   return hipGetLastError();
 }
+
+template hipError_t launch_sumsq(const PinnedList&, double*, hipStream_t);
+template hipError_t launch_sumsq(const ArgList&, double*, hipStream_t);
+template hipError_t launch_clip(const PinnedList&, const double*, uint32_t, float,
+                                tlc_norm_result*, hipStream_t);
+template hipError_t launch_clip(const ArgList&, const double*, uint32_t, float, tlc_norm_result*,
+                                hipStream_t);
 
 }  // namespace tlc

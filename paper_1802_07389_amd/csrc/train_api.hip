@@ -13,7 +13,10 @@ using namespace tlc;
 
 namespace {
 
-constexpr int kSlots = 4;
+// Staging slots of the lists' pieces, in two groups: one event after a group's
+// last call guards the group (an event a call cost the host more than the
+// pieces).
+constexpr int kGroups = 2, kGroupSlots = 4;
 constexpr size_t kMaxListValues = (size_t)1 << 40;
 
 bool known_type(int type) { return type == TLC_F32 || type == TLC_BF16 || type == TLC_F16; }
@@ -45,8 +48,8 @@ struct tlc_train {
   Piece* staging = nullptr;
   Piece* staging_dev = nullptr;  // the same, as the device addresses it
   size_t slot_pieces = 0;
-  hipEvent_t slot_done[kSlots] = {};
-  bool slot_used[kSlots] = {};
+  hipEvent_t group_done[kGroups] = {};
+  bool group_used[kGroups] = {};
   int slot_next = 0;
   // host tables, reserved at creation so that the calls do not allocate
   std::vector<Span> spans, spans_ok;
@@ -82,95 +85,133 @@ int check_table(const char* fn, size_t rows, size_t dim, int ids_type, int value
   return TLC_OK;
 }
 
-// A pinned slot, free once the kernels of its last call have run.
-int take_slot(tlc_train* c, int* slot) {
-  *slot = c->slot_next;
-  c->slot_next = (*slot + 1) % kSlots;
-  if (c->slot_used[*slot]) {
-    const hipError_t e = hipEventSynchronize(c->slot_done[*slot]);
+// The next pinned slot: a group's first one waits for the group's last calls.
+int take_slot(tlc_train* c, Piece** host, const Piece** dev) {
+  const int slot = c->slot_next, group = slot / kGroupSlots;
+  if (slot % kGroupSlots == 0 && c->group_used[group]) {
+    const hipError_t e = hipEventSynchronize(c->group_done[group]);
     if (e != hipSuccess) return hip_fail(e, "hipEventSynchronize(staging)");
-    c->slot_used[*slot] = false;
+    c->group_used[group] = false;
   }
+  *host = c->staging + (size_t)slot * c->slot_pieces;
+  *dev = c->staging_dev + (size_t)slot * c->slot_pieces;
   return TLC_OK;
 }
 
-// Checks a list of tensors and cuts it into pieces: into l's table, or into a
-// pinned slot (*slot, to be held after the kernels that read it; else -1).
-// clip: the tensors are scaled into outs, or in place (outs NULL).
-int cut_list(tlc_train* c, const char* fn, size_t count, const void* const* tensors,
-             const int* types, const size_t* ns, tlc_norm_result* result, bool clip,
-             float* const* outs, ListArgs* l, int* slot) {
-  *slot = -1;
+// After the kernels that read the slot are queued.
+int leave_slot(tlc_train* c) {
+  const int slot = c->slot_next, group = slot / kGroupSlots;
+  c->slot_next = (slot + 1) % (kGroups * kGroupSlots);
+  if (c->slot_next % kGroupSlots != 0) return TLC_OK;
+  const hipError_t e = hipEventRecord(c->group_done[group], c->stream);
+  if (e != hipSuccess) return launched(c, e, "hipEventRecord(staging)");
+  c->group_used[group] = true;
+  return TLC_OK;
+}
+
+// A call on a list of tensors.  clip: they are scaled into outs, or in place
+// (outs NULL).
+struct ListCall {
+  size_t count;
+  const void* const* tensors;
+  const int* types;
+  const size_t* ns;
+  tlc_norm_result* result;
+  bool clip;
+  float* const* outs;
+  size_t total = 0, bytes = 0;  // set by check_list
+};
+
+int check_list(tlc_train* c, const char* fn, ListCall* l) {
   int st = check_usable(c, fn);
   if (st) return st;
-  if (!result) return fail(TLC_E_INVALID, "%s: NULL result", fn);
-  if (count && (!tensors || !types || !ns)) return fail(TLC_E_INVALID, "%s: NULL argument", fn);
-  if (count > c->max_tensors)
-    return fail(TLC_E_INVALID, "%s: %zu tensors exceed the context's %zu", fn, count,
+  if (!l->result) return fail(TLC_E_INVALID, "%s: NULL result", fn);
+  if (l->count && (!l->tensors || !l->types || !l->ns))
+    return fail(TLC_E_INVALID, "%s: NULL argument", fn);
+  if (l->count > c->max_tensors)
+    return fail(TLC_E_INVALID, "%s: %zu tensors exceed the context's %zu", fn, l->count,
                 c->max_tensors);
-  size_t total = 0, total_bytes = 0;
   c->spans.clear();
-  add_span(c->spans, result, sizeof(*result), true);
-  for (size_t i = 0; i < count; ++i) {
-    if (ns[i] == 0) continue;
-    if (!known_type(types[i]))
-      return fail(TLC_E_INVALID, "%s: tensor %zu: unknown type %d", fn, i, types[i]);
-    if (ns[i] > TLC_MAX_N)
-      return fail(TLC_E_INVALID, "%s: tensor %zu: n = %zu too large", fn, i, ns[i]);
-    if (!tensors[i] || (outs && !outs[i]))
+  add_span(c->spans, l->result, sizeof(*l->result), true);
+  for (size_t i = 0; i < l->count; ++i) {
+    const size_t n = l->ns[i];
+    if (n == 0) continue;
+    if (!known_type(l->types[i]))
+      return fail(TLC_E_INVALID, "%s: tensor %zu: unknown type %d", fn, i, l->types[i]);
+    if (n > TLC_MAX_N)
+      return fail(TLC_E_INVALID, "%s: tensor %zu: n = %zu too large", fn, i, n);
+    if (!l->tensors[i] || (l->outs && !l->outs[i]))
       return fail(TLC_E_INVALID, "%s: tensor %zu: NULL pointer", fn, i);
-    total += ns[i];
-    const size_t bytes = ns[i] * type_bytes(types[i]);
-    total_bytes += bytes;
+    const size_t bytes = n * type_bytes(l->types[i]);
+    l->total += n;
+    l->bytes += bytes;
     const bool in_place =
-        clip && (!outs || ((const void*)outs[i] == tensors[i] && types[i] == TLC_F32));
-    add_span(c->spans, tensors[i], bytes, in_place);
-    if (clip && !in_place) add_span(c->spans, outs[i], ns[i] * 4, true);
+        l->clip &&
+        (!l->outs || ((const void*)l->outs[i] == l->tensors[i] && l->types[i] == TLC_F32));
+    add_span(c->spans, l->tensors[i], bytes, in_place);
+    if (l->clip && !in_place) add_span(c->spans, l->outs[i], n * 4, true);
   }
-  if (total > kMaxListValues)
-    return fail(TLC_E_INVALID, "%s: %zu values exceed %zu", fn, total, kMaxListValues);
+  if (l->total > kMaxListValues)
+    return fail(TLC_E_INVALID, "%s: %zu values exceed %zu", fn, l->total, kMaxListValues);
   if (spans_conflict_cached(c->spans, c->spans_ok))
     return fail(TLC_E_INVALID, "%s: a written buffer overlaps another one", fn);
-  l->own_type = clip && !outs;
-  l->stream = total_bytes > kCacheBytes;
-  l->len = (uint32_t)(std::max<size_t>(1, ceil_div(ceil_div(total, kNormBlocks), kPieceValues)) *
-                      kPieceValues);
-  if (count <= kArgTensors) {
-    for (size_t i = 0; i < count; ++i) {
-      if (ns[i] == 0) continue;
-      ListTensor& e = l->tensors[l->count++];
-      e.x = tensors[i];
-      e.out = outs ? (void*)outs[i] : (void*)tensors[i];
-      e.n = (uint32_t)ns[i];
-      e.piece0_type = l->n | (uint32_t)types[i] << 30;
-      l->n += (uint32_t)ceil_div(ns[i], l->len);
-    }
-    return TLC_OK;
-  }
-  st = take_slot(c, slot);
-  if (st) return st;
-  Piece* host = c->staging + (size_t)*slot * c->slot_pieces;
-  l->pieces = c->staging_dev + (size_t)*slot * c->slot_pieces;
-  for (size_t i = 0; i < count; ++i) {
-    const size_t size = type_bytes(types[i]);
-    for (size_t k = 0; k < ns[i]; k += l->len) {
-      Piece& p = host[l->n++];
-      p.x = (const uint8_t*)tensors[i] + k * size;
-      p.out = outs ? (void*)(outs[i] + k) : (void*)p.x;
-      p.n = (uint32_t)std::min<size_t>(l->len, ns[i] - k);
-      p.type = (uint32_t)types[i];
-    }
-  }
   return TLC_OK;
 }
 
-// The staging slot is free again once the kernels queued so far have run.
-int hold_slot(tlc_train* c, int slot) {
-  if (slot < 0) return TLC_OK;
-  const hipError_t e = hipEventRecord(c->slot_done[slot], c->stream);
-  if (e != hipSuccess) return launched(c, e, "hipEventRecord(staging)");
-  c->slot_used[slot] = true;
-  return TLC_OK;
+template <class List>
+List new_list(const ListCall& l) {
+  List r = {};
+  r.own_type = l.clip && !l.outs;
+  r.stream = l.bytes > kCacheBytes;
+  return r;
+}
+
+ArgList arg_list(const ListCall& l) {
+  ArgList r = new_list<ArgList>(l);
+  r.len = piece_values(l.total, l.count);
+  for (size_t i = 0; i < l.count; ++i) {
+    if (l.ns[i] == 0) continue;
+    ListTensor& e = r.tensors[r.count++];
+    e.x = l.tensors[i];
+    e.out = l.outs ? (void*)l.outs[i] : (void*)l.tensors[i];
+    e.n = (uint32_t)l.ns[i];
+    e.piece0_type = r.n | (uint32_t)l.types[i] << 30;
+    r.n += (uint32_t)ceil_div(l.ns[i], r.len);
+  }
+  return r;
+}
+
+PinnedList pinned_list(const ListCall& l, Piece* host, const Piece* dev) {
+  PinnedList r = new_list<PinnedList>(l);
+  r.pieces = dev;
+  const size_t len = piece_values(l.total, l.count);
+  for (size_t i = 0; i < l.count; ++i) {
+    const size_t size = type_bytes(l.types[i]);
+    for (size_t k = 0; k < l.ns[i]; k += len) {
+      Piece& p = host[r.n++];
+      p.x = (const uint8_t*)l.tensors[i] + k * size;
+      p.out = l.outs ? (void*)(l.outs[i] + k) : (void*)p.x;
+      p.n = (uint32_t)std::min<size_t>(len, l.ns[i] - k);
+      p.type = (uint32_t)l.types[i];
+    }
+  }
+  return r;
+}
+
+// Checks the call, then has `run` queue its kernels on the list.
+template <class F>
+int run_list(tlc_train* c, const char* fn, ListCall l, F&& run) {
+  int st = check_list(c, fn, &l);
+  if (st) return st;
+  DeviceScope dev(c->device);
+  st = dev.status();
+  if (st) return st;
+  if (l.count <= kArgTensors) return launched(c, run(arg_list(l)), fn);
+  Piece* host = nullptr;
+  const Piece* pieces = nullptr;
+  st = take_slot(c, &host, &pieces);
+  if (!st) st = launched(c, run(pinned_list(l, host, pieces)), fn);
+  return st ? st : leave_slot(c);
 }
 
 int check_clip(const char* fn, float max_norm) {
@@ -226,12 +267,12 @@ TLC_API int tlc_train_create(tlc_train** out, size_t max_tokens, size_t max_rows
   if (e == hipSuccess) e = hipHostMalloc((void**)&c->bad, 256, hipHostMallocDefault);
   if (e == hipSuccess) e = hipHostGetDevicePointer((void**)&c->bad_dev, c->bad, 0);
   if (e == hipSuccess && c->slot_pieces)
-    e = hipHostMalloc((void**)&c->staging, kSlots * c->slot_pieces * sizeof(Piece),
+    e = hipHostMalloc((void**)&c->staging, kGroups * kGroupSlots * c->slot_pieces * sizeof(Piece),
                       hipHostMallocDefault);
   if (e == hipSuccess && c->staging)
     e = hipHostGetDevicePointer((void**)&c->staging_dev, c->staging, 0);
-  for (int i = 0; i < kSlots && e == hipSuccess; ++i)
-    e = hipEventCreateWithFlags(&c->slot_done[i], hipEventDisableTiming);
+  for (int i = 0; i < kGroups && e == hipSuccess; ++i)
+    e = hipEventCreateWithFlags(&c->group_done[i], hipEventDisableTiming);
   if (e != hipSuccess) {
     tlc_train_destroy(c);
     return hip_fail(e, "tlc_train_create: workspace");
@@ -261,8 +302,8 @@ TLC_API int tlc_train_destroy(tlc_train* c) {
   if (!c) return TLC_OK;
   DeviceScope dev(c->device);
   (void)hipStreamSynchronize(c->stream);
-  for (int i = 0; i < kSlots; ++i)
-    if (c->slot_done[i]) (void)hipEventDestroy(c->slot_done[i]);
+  for (int i = 0; i < kGroups; ++i)
+    if (c->group_done[i]) (void)hipEventDestroy(c->group_done[i]);
   if (c->staging) (void)hipHostFree(c->staging);
   if (c->bad) (void)hipHostFree(c->bad);
   if (c->ws) (void)hipFree(c->ws);
@@ -372,51 +413,36 @@ TLC_API int tlc_embedding_grad(tlc_train* c, const void* grad, int grad_type, si
 // ---------------------------------------------------------------- norm, clip
 TLC_API int tlc_grad_norm(tlc_train* c, size_t count, const void* const* tensors,
                           const int* types, const size_t* ns, tlc_norm_result* result) {
-  const char* fn = "tlc_grad_norm";
-  ListArgs l = {};
-  int slot = -1;
-  int st = cut_list(c, fn, count, tensors, types, ns, result, false, nullptr, &l, &slot);
-  if (st) return st;
-  DeviceScope dev(c->device);
-  st = dev.status();
-  if (st) return st;
-  st = launched(c, launch_sumsq(l, c->partials, c->stream), fn);
-  if (!st)
-    st = launched(c, launch_norm_finish(c->partials, norm_blocks(l.n), result, c->stream), fn);
-  return st ? st : hold_slot(c, slot);
+  return run_list(c, "tlc_grad_norm", ListCall{count, tensors, types, ns, result, false, nullptr},
+                  [&](const auto& list) {
+                    const hipError_t e = launch_sumsq(list, c->partials, c->stream);
+                    if (e != hipSuccess) return e;
+                    return launch_norm_finish(c->partials, norm_blocks(list.n), result, c->stream);
+                  });
 }
 
 TLC_API int tlc_clip(tlc_train* c, size_t count, const void* const* tensors, const int* types,
                      const size_t* ns, float max_norm, tlc_norm_result* result,
                      float* const* outs) {
-  const char* fn = "tlc_clip";
-  ListArgs l = {};
-  int slot = -1;
-  int st = check_clip(fn, max_norm);
-  if (!st) st = cut_list(c, fn, count, tensors, types, ns, result, true, outs, &l, &slot);
+  const int st = check_clip("tlc_clip", max_norm);
   if (st) return st;
-  DeviceScope dev(c->device);
-  st = dev.status();
-  if (st) return st;
-  st = launched(c, launch_clip(l, nullptr, 0, max_norm, result, c->stream), fn);
-  return st ? st : hold_slot(c, slot);
+  return run_list(c, "tlc_clip", ListCall{count, tensors, types, ns, result, true, outs},
+                  [&](const auto& list) {
+                    return launch_clip(list, nullptr, 0, max_norm, result, c->stream);
+                  });
 }
 
 TLC_API int tlc_clip_grad_norm(tlc_train* c, size_t count, const void* const* tensors,
                                const int* types, const size_t* ns, float max_norm,
                                tlc_norm_result* result, float* const* outs) {
-  const char* fn = "tlc_clip_grad_norm";
-  ListArgs l = {};
-  int slot = -1;
-  int st = check_clip(fn, max_norm);
-  if (!st) st = cut_list(c, fn, count, tensors, types, ns, result, true, outs, &l, &slot);
+  const int st = check_clip("tlc_clip_grad_norm", max_norm);
   if (st) return st;
-  DeviceScope dev(c->device);
-  st = dev.status();
-  if (st) return st;
-  st = launched(c, launch_sumsq(l, c->partials, c->stream), fn);
-  if (!st)
-    st = launched(c, launch_clip(l, c->partials, norm_blocks(l.n), max_norm, result, c->stream),
-                  fn);
-  return st ? st : hold_slot(c, slot);
+  return run_list(c, "tlc_clip_grad_norm",
+                  ListCall{count, tensors, types, ns, result, true, outs},
+                  [&](const auto& list) {
+                    const hipError_t e = launch_sumsq(list, c->partials, c->stream);
+                    if (e != hipSuccess) return e;
+                    return launch_clip(list, c->partials, norm_blocks(list.n), max_norm, result,
+                                       c->stream);
+                  });
 }
