@@ -34,32 +34,28 @@ __device__ __forceinline__ uint32_t token_key(const EmbArgs& a, uint32_t t, bool
   return (uint32_t)id;
 }
 
-// Zeroes the rows of block b of the fill that no token touched; touched: marks
-// of the block's rows.
-template <uint32_t kBlock>
-__device__ __forceinline__ void fill_rows(const FillArgs& f, uint32_t b, const uint8_t* touched) {
-  const uint64_t r0 = (uint64_t)b * f.block_rows;
-  const uint32_t n = (uint32_t)umin64(f.block_rows, f.rows - r0) * f.packs.d;
-  float* out = f.out + r0 * f.out_stride;
-  constexpr uint32_t kMany = 8;  // marks asked for before the first store
-  for (uint32_t u0 = threadIdx.x; u0 < n; u0 += kMany * kBlock) {
-    uint32_t r[kMany];
-    bool skip[kMany];
-#pragma unroll
-    for (uint32_t i = 0; i < kMany; ++i) {
-      r[i] = quotient(umin32(u0 + i * kBlock, n - 1), f.packs);
-      skip[i] = touched[r[i]] || u0 + i * kBlock >= n;
-    }
-#pragma unroll
-    for (uint32_t i = 0; i < kMany; ++i) {
-      if (skip[i]) continue;
-      float* o = out + r[i] * f.out_stride;
-      const uint32_t j = u0 + i * kBlock - r[i] * f.packs.d;
-      if (f.dim >= 4)
-        st_stream(o + umin32(j * 4, f.dim - 4), make_float4(0.0f, 0.0f, 0.0f, 0.0f));
-      else
-        o[j] = 0.0f;
-    }
+// Pack j of a row of the fill.
+__device__ __forceinline__ void zero_pack(const FillArgs& f, uint64_t row, uint32_t j) {
+  float* o = f.out + row * f.out_stride;
+  if (f.dim >= 4)
+    st_stream(o + umin32(j * 4, f.dim - 4), make_float4(0.0f, 0.0f, 0.0f, 0.0f));
+  else
+    o[j] = 0.0f;
+}
+
+// Zeroes the rows that no token touched: block `i` of the launch's fill, a pack a
+// thread at a time (tiles of f.tile_rows rows, or f.row_tiles tiles of a row), so
+// that all blocks together write one range after the other (64 KB a block
+// instead: 327 against 298 us for a gradient of 1 GiB of 131072 tokens).
+__device__ __forceinline__ void fill_rows(const FillArgs& f, uint32_t i) {
+  for (uint32_t b = f.tile0 + i; b < f.tile1; b += f.blocks) {
+    const bool split = f.row_tiles.d > 1;
+    const uint32_t q = split ? quotient(b, f.row_tiles) : 0u;
+    const uint64_t r0 = split ? q : (uint64_t)b * f.tile_rows;
+    const uint32_t u = split ? (b - q * f.row_tiles.d) * kSortThreads + threadIdx.x : threadIdx.x;
+    const uint32_t r = quotient(u, f.packs);
+    if (r >= f.tile_rows || r0 + r >= f.rows) continue;
+    if (!f.touched[r0 + r]) zero_pack(f, r0 + r, u - r * f.packs.d);
   }
 }
 
@@ -161,8 +157,7 @@ __global__ __launch_bounds__(kSortThreads) void tlc_token_count_kernel(
     EmbArgs a, SortArgs s, uint32_t* __restrict__ keys, uint8_t* __restrict__ touched,
     FillArgs f) {
   if (blockIdx.x >= s.tiles) {
-    const uint32_t b = f.block0 + blockIdx.x - s.tiles;
-    fill_rows<kSortThreads>(f, b, f.touched + (uint64_t)b * f.block_rows);
+    fill_rows(f, blockIdx.x - s.tiles);
     return;
   }
   __shared__ uint32_t n[kDigits];
@@ -202,8 +197,7 @@ __global__ __launch_bounds__(kSortThreads) void tlc_token_sort_kernel(SortArgs s
   __shared__ uint32_t scan_lds[kW];
   __shared__ uint32_t next[kNext ? kNextTiles * kDigits : 1];
   if (blockIdx.x >= s.tiles) {
-    const uint32_t b = f.block0 + blockIdx.x - s.tiles;
-    fill_rows<kSortThreads>(f, b, f.touched + (uint64_t)b * f.block_rows);
+    fill_rows(f, blockIdx.x - s.tiles);
     return;
   }
   static_assert(kDigits == kSortThreads, "a digit a thread");
@@ -285,7 +279,7 @@ __device__ __forceinline__ void put_row_over(const EmbArgs& a, float* p, Pack<fl
                                              const float* v) {
 #pragma unroll
   for (int i = 0; i < V; ++i) o.set(i, kAdd ? o.get(i) + a.scale * v[i] : a.scale * v[i]);
-  store_pack<float, V>(p, o);
+  store_pack<float, V, true>(p, o);
 }
 template <int V, bool kAdd>
 __device__ __forceinline__ void put_row(const EmbArgs& a, uint32_t row, uint32_t k,
@@ -411,7 +405,7 @@ struct WaveRuns {
 
 // Few tokens in one launch, without a partial row: every block sorts all of
 // them, and takes the runs that begin in its share of the sorted tokens, its
-// waves an equal part each.  Blocks from `blocks` * `slabs` on look at all ids and
+// waves an equal part each.  Blocks from s.blocks * s.slabs on look at all ids and
 // fill rows.
 template <class In, int V, bool kAdd, int kItems>
 __global__ __launch_bounds__(kSmallThreads) void tlc_embedding_grad_small_kernel(
@@ -429,16 +423,27 @@ __global__ __launch_bounds__(kSmallThreads) void tlc_embedding_grad_small_kernel
   __shared__ uint32_t scan_lds[kW], head[kW], span[2];
   const uint32_t lane = threadIdx.x & 63u, wid = uniform32(threadIdx.x >> 6);
   if (blockIdx.x >= s.blocks * s.slabs) {
+    // groups of f.group rows, f.blocks groups apart: all blocks together write
+    // one range after the other
     const uint32_t b = blockIdx.x - s.blocks * s.slabs;
-    const uint64_t r0 = (uint64_t)b * f.block_rows;
-    for (uint32_t r = threadIdx.x; r < f.block_rows; r += kSmallThreads) lds.marks[r] = 0;
+    for (uint32_t r = threadIdx.x; r < kSmallFillRows; r += kSmallThreads) lds.marks[r] = 0;
     __syncthreads();
     for (uint32_t t = threadIdx.x; t < a.count; t += kSmallThreads) {
       const uint32_t key = token_key(a, t, false);
-      if (key < a.rows && key - r0 < f.block_rows) lds.marks[key - r0] = 1;
+      if (key >= a.rows) continue;
+      const uint32_t g = quotient(key, f.group), k = quotient(g, f.stride);
+      if (g - k * f.stride.d == b) lds.marks[k * f.group.d + key - g * f.group.d] = 1;
     }
     __syncthreads();
-    fill_rows<kSmallThreads>(f, b, lds.marks);
+    uint32_t k = 0;
+    for (uint64_t g = b; g * f.group.d < f.rows; g += f.stride.d, ++k) {
+      const uint64_t r0 = g * f.group.d;
+      const uint32_t n = (uint32_t)umin64(f.group.d, f.rows - r0) * f.packs.d;
+      for (uint32_t u = threadIdx.x; u < n; u += kSmallThreads) {
+        const uint32_t r = quotient(u, f.packs);
+        if (!lds.marks[k * f.group.d + r]) zero_pack(f, r0 + r, u - r * f.packs.d);
+      }
+    }
     return;
   }
   const uint32_t block = blockIdx.x / s.slabs, slab = blockIdx.x % s.slabs;
@@ -573,12 +578,13 @@ __global__ __launch_bounds__(kJoinThreads) void tlc_embedding_grad_join_kernel(
 
 namespace {
 
-// Blocks of the fill for one launch: out of those that are left, a share.
-uint32_t take_fill(FillArgs* f, uint32_t* left, uint32_t launches) {
-  const uint32_t n = *left / launches;
-  f->block0 = f->blocks - *left;
-  *left -= n;
-  return n;
+// The next launch's share of the fill: of what is left to `launches` launches.
+// Returns its blocks.
+uint32_t take_fill(FillArgs* f, uint32_t launches) {
+  f->tile0 = f->tile1;
+  f->tile1 += (f->tiles - f->tile0) / launches;
+  f->blocks = std::min(f->tile1 - f->tile0, kFillBlocks);
+  return f->blocks;
 }
 
 // Sorts the tokens, and fills beside; returns which of w.keys and w.pos hold
@@ -589,9 +595,8 @@ int sort_tokens(const EmbArgs& a, const GradWork& w, uint32_t passes, FillArgs f
   SortArgs s = {};
   s.count = a.count;
   s.tiles = (a.count + kTile - 1) / kTile;
-  uint8_t* touched = f.blocks ? w.touched : nullptr;
+  uint8_t* touched = f.tiles ? w.touched : nullptr;
   const bool next = s.tiles <= kNextTiles;  // a pass counts for the one after it
-  uint32_t left = f.blocks;
   uint32_t launches = next ? passes : 2 * passes - 1;  // that take a share of the fill
   for (uint32_t p = 0; p < passes; ++p) {
     s.keys_in = w.keys[p & 1];
@@ -604,11 +609,11 @@ int sort_tokens(const EmbArgs& a, const GradWork& w, uint32_t passes, FillArgs f
     s.shift = p * kDigitBits;
     if (p == 0 || !next) {
       // no fill beside the first count, which makes the marks
-      const uint32_t fill = p ? take_fill(&f, &left, launches--) : 0;
+      const uint32_t fill = p ? take_fill(&f, launches--) : 0;
       launch_k(tlc_token_count_kernel<kItems>, s.tiles + fill, kSortThreads, st, a, s, w.keys[0],
                touched, f);
     }
-    const uint32_t fill = take_fill(&f, &left, launches--);
+    const uint32_t fill = take_fill(&f, launches--);
     if (s.next)
       launch_k(tlc_token_sort_kernel<kItems, true>, s.tiles + fill, kSortThreads, st, s, f);
     else
@@ -632,10 +637,20 @@ void launch_grad(const EmbArgs& a, const GradWork& w, hipStream_t st) {
     f.rows = a.rows;
     f.dim = a.dim;
     f.packs = divider(packs);
-    f.block_rows = std::max(1u, kFillPacks / packs);
-    if (small)  // a block looks at all ids: at most about kSmallFillBlocks of them
-      f.block_rows = std::min(std::max(f.block_rows, a.rows / kSmallFillBlocks), kSmallFillRows);
-    f.blocks = (a.rows + f.block_rows - 1) / f.block_rows;
+    if (small) {
+      const uint32_t group = std::max(1u, std::min(kSmallThreads / packs, a.rows));
+      const uint32_t groups = (a.rows + group - 1) / group;
+      // a block looks at all ids: few blocks, but marks for all of its rows
+      f.blocks = std::min(groups, std::max(kSmallFillBlocks,
+                                           groups / (kSmallFillRows / group) + 1));
+      f.group = divider(group);
+      f.stride = divider(f.blocks);
+    } else {
+      f.tile_rows = std::max(1u, kSortThreads / packs);
+      const uint32_t row_tiles = (packs + kSortThreads - 1) / kSortThreads;
+      f.row_tiles = divider(row_tiles);
+      f.tiles = row_tiles > 1 ? a.rows * row_tiles : (a.rows + f.tile_rows - 1) / f.tile_rows;
+    }
   }
   SumArgs s = {};
   s.parts = w.parts;
@@ -677,9 +692,11 @@ hipError_t launch_embedding_grad(const EmbArgs& a, int grad_type, bool accumulat
                                  const GradWork& w, hipStream_t st) {
   with_type(grad_type, [&](auto in) {
     using In = decltype(in);
-    constexpr int V = 16 / sizeof(In);
-    if (a.dim >= V)
-      accumulate ? launch_grad<In, V, true>(a, w, st) : launch_grad<In, V, false>(a, w, st);
+    // 16 bytes of the output a lane, so that a wave's stores fill whole lines
+    // (bf16 gradients in packs of eight, two stores a lane: 74.4 instead of 67.3
+    // us for 60000 tokens of 512 added to 50000 rows)
+    if (a.dim >= 4)
+      accumulate ? launch_grad<In, 4, true>(a, w, st) : launch_grad<In, 4, false>(a, w, st);
     else
       accumulate ? launch_grad<In, 1, true>(a, w, st) : launch_grad<In, 1, false>(a, w, st);
   });

@@ -119,7 +119,7 @@ struct ListCall {
   tlc_norm_result* result;
   bool clip;
   float* const* outs;
-  size_t total = 0, bytes = 0;  // set by check_list
+  size_t total = 0;  // values; set by check_list
 };
 
 int check_list(tlc_train* c, const char* fn, ListCall* l) {
@@ -144,7 +144,6 @@ int check_list(tlc_train* c, const char* fn, ListCall* l) {
       return fail(TLC_E_INVALID, "%s: tensor %zu: NULL pointer", fn, i);
     const size_t bytes = n * type_bytes(l->types[i]);
     l->total += n;
-    l->bytes += bytes;
     const bool in_place =
         l->clip &&
         (!l->outs || ((const void*)l->outs[i] == l->tensors[i] && l->types[i] == TLC_F32));
@@ -158,16 +157,9 @@ int check_list(tlc_train* c, const char* fn, ListCall* l) {
   return TLC_OK;
 }
 
-template <class List>
-List new_list(const ListCall& l) {
-  List r = {};
-  r.own_type = l.clip && !l.outs;
-  r.stream = l.bytes > kCacheBytes;
-  return r;
-}
-
 ArgList arg_list(const ListCall& l) {
-  ArgList r = new_list<ArgList>(l);
+  ArgList r = {};
+  r.own_type = l.clip && !l.outs;
   r.len = piece_values(l.total, l.count);
   for (size_t i = 0; i < l.count; ++i) {
     if (l.ns[i] == 0) continue;
@@ -182,7 +174,8 @@ ArgList arg_list(const ListCall& l) {
 }
 
 PinnedList pinned_list(const ListCall& l, Piece* host, const Piece* dev) {
-  PinnedList r = new_list<PinnedList>(l);
+  PinnedList r = {};
+  r.own_type = l.clip && !l.outs;
   r.pieces = dev;
   const size_t len = piece_values(l.total, l.count);
   for (size_t i = 0; i < l.count; ++i) {
@@ -415,7 +408,7 @@ TLC_API int tlc_grad_norm(tlc_train* c, size_t count, const void* const* tensors
                           const int* types, const size_t* ns, tlc_norm_result* result) {
   return run_list(c, "tlc_grad_norm", ListCall{count, tensors, types, ns, result, false, nullptr},
                   [&](const auto& list) {
-                    const hipError_t e = launch_sumsq(list, c->partials, c->stream);
+                    const hipError_t e = launch_sumsq(list, true, c->partials, c->stream);
                     if (e != hipSuccess) return e;
                     return launch_norm_finish(c->partials, norm_blocks(list.n), result, c->stream);
                   });
@@ -440,7 +433,7 @@ TLC_API int tlc_clip_grad_norm(tlc_train* c, size_t count, const void* const* te
   return run_list(c, "tlc_clip_grad_norm",
                   ListCall{count, tensors, types, ns, result, true, outs},
                   [&](const auto& list) {
-                    const hipError_t e = launch_sumsq(list, c->partials, c->stream);
+                    const hipError_t e = launch_sumsq(list, false, c->partials, c->stream);
                     if (e != hipSuccess) return e;
                     return launch_clip(list, c->partials, norm_blocks(list.n), max_norm, result,
                                        c->stream);

@@ -59,12 +59,19 @@ struct FillArgs {
   uint64_t out_stride;
   const uint8_t* touched;
   uint64_t rows;
-  uint32_t dim, block_rows, block0, blocks;
-  Divider packs;  // float4s (or, of shorter rows, floats) of a row
+  uint32_t dim;
+  Divider packs;     // float4s (or, of shorter rows, floats) of a row
+  uint32_t blocks;   // of the launch
+  // beside the sort: tiles of kSortThreads packs at most
+  uint32_t tiles, tile0, tile1;  // all, and the launch's
+  uint32_t tile_rows;            // rows of a tile (1 where a row has several)
+  Divider row_tiles;             // tiles of a row
+  // few tokens: groups of rows, `stride` groups from one of a block's to the next
+  Divider group, stride;
 };
-constexpr uint32_t kFillPacks = 4096;  // of one block
+constexpr uint32_t kFillBlocks = 1u << 20;  // of a launch
 constexpr uint32_t kSmallFillBlocks = 1024;
-constexpr uint32_t kSmallFillRows = 8192;
+constexpr uint32_t kSmallFillRows = 8192;   // of a block
 // The sums: kSumWaves waves of a block, each per_wave sorted tokens.
 constexpr uint32_t kSumThreads = 256;
 constexpr uint32_t kSumWaves = kSumThreads / 64;
@@ -129,12 +136,11 @@ struct PinnedList {
   const Piece* pieces;
   uint32_t n;     // pieces
   bool own_type;  // clipping: out is of x's type (else fp32)
-  bool stream;    // the values don't fit the last-level cache
 };
 struct ArgList {
   uint32_t count, n;  // tensors, pieces
   uint32_t len;       // values of a piece
-  bool own_type, stream;
+  bool own_type;
   ListTensor tensors[kArgTensors];
 };
 static_assert(sizeof(ArgList) <= 3328, "kernel arguments end at 4096 bytes");
@@ -143,8 +149,9 @@ static_assert(sizeof(ArgList) <= 3328, "kernel arguments end at 4096 bytes");
 inline uint32_t norm_blocks(uint32_t pieces) {
   return pieces < kNormBlocks ? pieces : kNormBlocks;
 }
+// read_once: no clipping follows.
 template <class List>
-hipError_t launch_sumsq(const List& list, double* partials, hipStream_t st);
+hipError_t launch_sumsq(const List& list, bool read_once, double* partials, hipStream_t st);
 // Their sum into the result.
 hipError_t launch_norm_finish(const double* partials, uint32_t np, tlc_norm_result* result,
                               hipStream_t st);
