@@ -266,10 +266,12 @@ int tlc_compress_noalloc(const float* tensor, float* residual, size_t n, float s
  * They run on a context of their own, bound to one HIP stream like a tlc_ctx:
  * asynchronous on that stream, no device memory allocated per call, tensors
  * device memory owned by the caller, the same rules for host threads and
- * errors.  The calls with ids may be captured into a graph; those over lists
- * of tensors hand their descriptors over in host memory that later calls use
- * again, and may not. */
+ * errors.  Their calls may be captured into a graph (lists of tensors: up to
+ * TLC_CAPTURE_TENSORS; longer ones are handed over in host memory that later
+ * calls use again, and refused).  tlc_profile_* does not time them. */
 typedef struct tlc_train tlc_train;
+
+#define TLC_CAPTURE_TENSORS 128
 
 /* Types of values and of token ids. */
 #define TLC_F32 0

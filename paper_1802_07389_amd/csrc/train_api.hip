@@ -200,6 +200,13 @@ int run_list(tlc_train* c, const char* fn, ListCall l, F&& run) {
   st = dev.status();
   if (st) return st;
   if (l.count <= kArgTensors) return launched(c, run(arg_list(l)), fn);
+  // a replay would read the slot after later calls have filled it again
+  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+  const hipError_t e = hipStreamIsCapturing(c->stream, &capture);
+  if (e != hipSuccess) return hip_fail(e, "hipStreamIsCapturing");
+  if (capture != hipStreamCaptureStatusNone)
+    return fail(TLC_E_INVALID, "%s: a list of %zu tensors cannot be captured (%u at most)", fn,
+                l.count, kArgTensors);
   Piece* host = nullptr;
   const Piece* pieces = nullptr;
   st = take_slot(c, &host, &pieces);

@@ -125,7 +125,7 @@ inline uint32_t piece_values(size_t total, size_t count) {
 // How the kernels are given a list: up to kArgTensors tensors with their
 // arguments, and a block finds its piece there; of more, the pieces are read in
 // pinned host memory.
-constexpr uint32_t kArgTensors = 128;
+constexpr uint32_t kArgTensors = TLC_CAPTURE_TENSORS;
 struct ListTensor {
   const void* x;
   void* out;

@@ -65,6 +65,7 @@ TLC_I32 = 0
 TLC_I64 = 1
 TLC_MAX_ROWS = 2147483646
 TLC_MAX_DIM = 16777216
+TLC_CAPTURE_TENSORS = 128
 
 EXPORTS = (
     "tlc_max_compressed_bytes", "tlc_ctx_create", "tlc_ctx_create_batch",

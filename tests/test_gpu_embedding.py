@@ -4,7 +4,7 @@ Bars.  Lookup: bit for bit the fp32 product rounded once (torch's own
 conversions on the CPU round half to even).  Gradient: a sum of m terms in
 fp32 in any order, one product and one addition are off by at most
 (m + 2) * 2^-24 * (scale * sum |x| + |out|), with 1 % for the higher orders
-(m < 2^17); rows without a token are exact.
+(m < 2^18.4); rows without a token are exact.
 """
 import numpy as np
 import pytest
@@ -255,6 +255,18 @@ def test_grad_table_heights(ctx, rows):
     for count in (300, 6000, 50000):
         check_grad(ctx, rng, count, rows, 33, "f32", "uniform")
         check_grad(ctx, rng, count, rows, 33, "f32", "ends", accumulate=True)
+
+
+@pytest.mark.parametrize("count", [(1 << 18) + 3, 300_001])
+def test_grad_many_tokens(count):
+    """Above 2^18 tokens the sort's tiles are wider."""
+    rng = np.random.default_rng([8, count])
+    with T().TrainContext(max_tokens=count, max_rows=1 << 20, max_dim=40) as c:
+        for rows, dim, kind in ((1000, 8, "zipf"), (70_001, 40, "uniform"), (300, 3, "same"),
+                                (1 << 20, 20, "zipf"), (9, 24, "few")):
+            check_grad(c, rng, count, rows, dim, "f32", kind)
+            check_grad(c, rng, count, rows, dim, "bf16", kind, "i32", padding=0,
+                       accumulate=True)
 
 
 def test_grad_all_tokens_invalid(ctx):

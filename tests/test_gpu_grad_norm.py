@@ -220,6 +220,42 @@ def test_other_stream():
         assert near(r.norm, math.sqrt(sumsq_of(ts)), ROUND)
 
 
+def test_capture():
+    """A captured norm and clip follow their tensors' new values, with eager
+    calls between the replays; longer lists refuse to be captured."""
+    tlc = T()
+    s = torch.cuda.Stream()
+    with tlc.TrainContext(max_tensors=500, stream=s) as c:
+        with torch.cuda.stream(s):
+            ts = tensors_of(7, [50_000, 3, 70_001], ("bf16", "f32"))
+            outs = [torch.empty(t.numel(), device="cuda") for t in ts]
+            many = c.tensor_list(tensors_of(8, [10] * 129, ("f32",)))
+            r, other = c.norm_result(), c.norm_result()
+            kept = c.tensor_list(ts, outs)
+            c.clip_grad_norm(kept, 0.1, result=r)
+            c.grad_norm(many, result=other)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            c.clip_grad_norm(kept, 0.1, result=r)
+            with pytest.raises(tlc.TLCError) as e:
+                c.grad_norm(many, result=other)
+        assert e.value.code == tlc.TLC_E_INVALID
+        for k in range(4):
+            with torch.cuda.stream(s):
+                for t in ts:
+                    t.mul_(1.25)
+                c.grad_norm(many, result=other)
+                for o in outs:
+                    o.fill_(float("nan"))
+                g.replay()
+            torch.cuda.synchronize()
+            want = math.sqrt(sumsq_of(ts))
+            assert near(r.norm, want, ROUND), k
+            assert near(r.coef, min(1.0, float(np.float32(0.1)) / want), ROUND)
+            assert all(bits_equal(o, r.coef * t.float()) for t, o in zip(ts, outs))
+
+
 def test_refusals(ctx):
     tlc = T()
     x, y = torch.randn(64, device="cuda"), torch.randn(64, device="cuda")
