@@ -669,8 +669,9 @@ void launch_grad(const EmbArgs& a, const GradWork& w, hipStream_t st) {
                passes, f);
     return;
   }
-  const int at = a.count > kWideTileTokens ? sort_tokens<16>(a, w, passes, f, st)
-                                           : sort_tokens<4>(a, w, passes, f, st);
+  const int at = a.count >= kTile16Tokens  ? sort_tokens<16>(a, w, passes, f, st)
+                 : a.count >= kTile4Tokens ? sort_tokens<4>(a, w, passes, f, st)
+                                           : sort_tokens<2>(a, w, passes, f, st);
   s.keys = w.keys[at];
   s.pos = w.pos[at];
   s.per_wave = sum_per_wave(a.count, s.slabs);

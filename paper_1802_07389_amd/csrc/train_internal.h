@@ -28,21 +28,28 @@ hipError_t launch_embedding(const EmbArgs& a, int table_type, int ids_type, int 
 
 // The gradient's sort by digits of the tokens' rows (heights below 2^18 in two
 // passes).  Up to kSmallTokens tokens every block of the sums sorts them in LDS;
-// more are sorted first, in tiles of four tokens a thread, above kWideTileTokens
-// of sixteen (every tile's block reads the counts of all).
+// more are sorted first, in tiles of two tokens a thread, from kTile4Tokens on of
+// four and from kTile16Tokens on of sixteen: small tiles fill the chip, but every
+// tile's block reads the counts of all (two | four | sixteen a thread: 30000
+// tokens 43.4 | 45.1 | 62.7 us, 130000 52.7 | 47.8 | 66.2, 500000 125 | 100 | 120,
+// 2000000 781 | 385 | 272).
 constexpr uint32_t kDigitBits = 9;
 constexpr uint32_t kDigits = 1u << kDigitBits;
 constexpr uint32_t kSortThreads = 512;
-constexpr uint32_t kSortTile = kSortThreads * 4;
+constexpr uint32_t kSortTile = kSortThreads * 2;  // the smallest
 constexpr uint32_t kSmallThreads = 1024;
 // (One launch | sorted first: 1000 tokens of 512 bf16 values added, common ids
 // 9.9 | 22.5 us, three ids in all 17.0 | 22.2; 2000 14.5 | 25.4 and 27.8 | 24.1;
 // 4000 26.9 | 27.5 and 54.0 | 26.7.)
 constexpr uint32_t kSmallTokens = kSmallThreads * 2;
 constexpr uint32_t kSortPasses = 4;  // at most, of 31 bits
+// Up to kNextTiles tiles a pass counts the next one's digits, which saves that
+// pass's count (16000 tokens 28.2 | 29.9 us; 28 tiles, whose counters hold up the
+// blocks that fill beside, 16384 tokens 68.6 instead of 62.9).
 constexpr uint32_t kNextTiles = 16;
 constexpr uint32_t kXcds = 8;
-constexpr uint32_t kWideTileTokens = 1u << 18;
+constexpr uint32_t kTile4Tokens = 1u << 16;
+constexpr uint32_t kTile16Tokens = 1u << 20;
 struct SortArgs {
   const uint32_t* keys_in;
   const uint32_t* pos_in;  // NULL: the tokens in their order
@@ -76,7 +83,7 @@ constexpr uint32_t kSmallFillRows = 8192;   // of a block
 constexpr uint32_t kSumThreads = 256;
 constexpr uint32_t kSumWaves = kSumThreads / 64;
 constexpr uint32_t kSumMinTokens = 16, kSumMaxTokens = 64;  // of a wave
-constexpr uint32_t kJoinThreads = 512;
+constexpr uint32_t kJoinThreads = 256;
 struct SumArgs {
   const uint32_t* keys;  // sorted; `rows` and above: adds nothing
   const uint32_t* pos;

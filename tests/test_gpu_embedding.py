@@ -257,9 +257,9 @@ def test_grad_table_heights(ctx, rows):
         check_grad(ctx, rng, count, rows, 33, "f32", "ends", accumulate=True)
 
 
-@pytest.mark.parametrize("count", [(1 << 18) + 3, 300_001])
+@pytest.mark.parametrize("count", [(1 << 16) - 1, 1 << 16, 300_001])
 def test_grad_many_tokens(count):
-    """Above 2^18 tokens the sort's tiles are wider."""
+    """Around the sizes at which the sort's tiles grow."""
     rng = np.random.default_rng([8, count])
     with T().TrainContext(max_tokens=count, max_rows=1 << 20, max_dim=40) as c:
         for rows, dim, kind in ((1000, 8, "zipf"), (70_001, 40, "uniform"), (300, 3, "same"),
@@ -267,6 +267,16 @@ def test_grad_many_tokens(count):
             check_grad(c, rng, count, rows, dim, "f32", kind)
             check_grad(c, rng, count, rows, dim, "bf16", kind, "i32", padding=0,
                        accumulate=True)
+
+
+@pytest.mark.parametrize("count", [(1 << 20) - 1, (1 << 20) + 1])
+def test_grad_a_million_tokens(count):
+    rng = np.random.default_rng([9, count])
+    with T().TrainContext(max_tokens=count, max_rows=1 << 18, max_dim=12) as c:
+        for rows, dim, kind in ((1000, 8, "zipf"), (1 << 18, 12, "uniform"), (511, 4, "sorted"),
+                                (99_999, 5, "descending")):
+            check_grad(c, rng, count, rows, dim, "f16", kind)
+            check_grad(c, rng, count, rows, dim, "f32", kind, "i32", accumulate=True)
 
 
 def test_grad_all_tokens_invalid(ctx):
