@@ -12,6 +12,12 @@
 // tokens is spread over the chip like any other, no atomics order anything,
 // and the bits depend on the sizes and ids alone.  Rows without a token are
 // zeroed by blocks beside the sorting ones, which leave the memory idle.
+//
+// 131072 tokens of 2048 bf16 values into 131072 rows (537 MB read, 1.07 GB
+// written): 295 us, 5.5 TB/s, of which the sums and their rows 155, the zeroes and
+// the sort beside them 130.  16384 tokens of 1024 values into 65536 rows: 61 us.
+// 10007 tokens of 515 fp16 values added to what is there: 29 us, five launches one
+// after the other, most of it their latency.
 #include "device_common.hpp"
 #include "train_internal.h"
 #include "typed_io.hpp"
@@ -403,7 +409,8 @@ struct WaveRuns {
 
 }  // namespace
 
-// Few tokens in one launch, without a partial row: every block sorts all of
+// Few tokens in one launch, without a partial row (512 tokens of 256 fp32 values,
+// 8 MB of rows set: 6.5 us, sorted first 23): every block sorts all of
 // them, and takes the runs that begin in its share of the sorted tokens, its
 // waves an equal part each.  Blocks from s.blocks * s.slabs on look at all ids and
 // fill rows.
@@ -478,7 +485,9 @@ __global__ __launch_bounds__(kSmallThreads) void tlc_embedding_grad_small_kernel
   if (runs.tail) runs.template finish<kW>(a, lds.heads, head, wid, col);
 }
 
-// Every wave: `per_wave` sorted tokens of one slab of columns.  What the block
+// Every wave: `per_wave` sorted tokens of one slab of columns, whose rows it asks
+// for eight at a time.  Bounded by the rows' bytes, read and written at 5 TB/s
+// together where there are many.  What the block
 // adds to a run that began earlier is its head, what it has of one that goes
 // on its tail: partial rows for the join.
 template <class In, int V, bool kAdd>
@@ -627,7 +636,9 @@ void launch_grad(const EmbArgs& a, const GradWork& w, hipStream_t st) {
   // passes over the bits of 0 .. rows
   const uint32_t bits = 32 - (uint32_t)__builtin_clz(a.rows);
   const uint32_t passes = (bits + kDigitBits - 1) / kDigitBits;
-  const bool small = a.count <= kSmallTokens;
+  const bool small =
+      a.count == 0 || (a.count <= kSmallTokens &&
+                       (kAdd || (uint64_t)a.rows * a.dim <= kSmallFillValues));
   FillArgs f = {};
   if (!kAdd) {
     const uint32_t packs = a.dim >= 4 ? (a.dim + 3) / 4 : a.dim;
@@ -664,8 +675,11 @@ void launch_grad(const EmbArgs& a, const GradWork& w, hipStream_t st) {
     if (a.count <= kSmallThreads)
       launch_k(tlc_embedding_grad_small_kernel<In, V, kAdd, 1>, grid, kSmallThreads, st, a, s,
                passes, f);
-    else
+    else if (a.count <= kSmallThreads * 2)
       launch_k(tlc_embedding_grad_small_kernel<In, V, kAdd, 2>, grid, kSmallThreads, st, a, s,
+               passes, f);
+    else
+      launch_k(tlc_embedding_grad_small_kernel<In, V, kAdd, 4>, grid, kSmallThreads, st, a, s,
                passes, f);
     return;
   }

@@ -1,4 +1,15 @@
 // norm.hip -- the global norm of a list of tensors, and their clipping.
+//
+//   sumsq = sum x^2,  norm = sqrt(sumsq),  coef = norm > max ? max / norm : 1,  out = coef * x
+//
+// What bounds it: the values read once for the norm, and once more to be clipped,
+// for which the last-level cache keeps what it can.  Squares and sums are in 64
+// bits: the conversions and multiply-adds hide behind the loads (2^28 fp32 values
+// in 159 us, 6.7 TB/s; with fp32 sums as fast, 480M bf16 values 150 against 144),
+// no value overflows, and the order of the sums, fixed by the sizes, does not
+// reach the norm's bits.  A partial sum a block and a second launch that adds
+// them: letting the block that is done last do so costs every block a fence and
+// an addition to one word (2^28 values 247 us, 25M 113 against 20).
 #include <type_traits>
 
 #include "device_common.hpp"
@@ -34,7 +45,7 @@ struct Clip {
 __device__ __forceinline__ Clip clip_of(double sumsq, float max_norm) {
   const double norm = sqrt(sumsq);
   Clip c;
-  c.finite = sumsq <= DBL_MAX;  // false for NaN too
+  c.finite = sumsq >= 0.0 && sumsq <= DBL_MAX;  // false for NaN too
   c.norm = (float)norm;
   c.coef = !c.finite ? __builtin_nanf("")
                      : (norm > (double)max_norm ? (float)((double)max_norm / norm) : 1.0f);
@@ -137,6 +148,7 @@ __device__ __forceinline__ void piece_scale(const Piece& p, float coef) {
 
 }  // namespace
 
+// Partial sums of squares, eight packs of 16 bytes a thread in flight.
 template <class List, bool kStream>
 __global__ __launch_bounds__(kNormThreads) void tlc_sumsq_kernel(List list,
                                                                  double* __restrict__ partials) {
@@ -166,13 +178,21 @@ __global__ __launch_bounds__(kNormThreads) void tlc_norm_finish_kernel(
   put_result(result, clip_of(sumsq, INFINITY));
 }
 
-// Out: float, or void: the tensors' own types.
+// The clipped tensors.  Out: float, or void: the tensors' own types.  100M bf16
+// values to fp32: 161 us with the norm (200 MB read twice, 400 MB written); 335
+// tensors of 1.7M values in all 14 us, of which two launches and a read of the
+// pieces over the bus are most.
 template <class List, class Out>
 __global__ __launch_bounds__(kNormThreads) void tlc_clip_kernel(
     List list, const double* __restrict__ partials, uint32_t np, float max_norm,
     tlc_norm_result* __restrict__ result) {
   constexpr bool kOwn = __is_same(Out, void);
   __shared__ double lds[kWaves];
+  const uint32_t p0 = (uint32_t)((uint64_t)blockIdx.x * list.n / gridDim.x);
+  const uint32_t p1 = (uint32_t)((uint64_t)(blockIdx.x + 1) * list.n / gridDim.x);
+  // asked for before the sums are there: it may be in host memory
+  Piece p = {};
+  if (p0 < p1) p = piece_of(list, p0);
   // sumsq is read by every block; the first one writes the rest
   const double sumsq = partials ? sum_partials(partials, np, lds) : result->sumsq;
   const Clip c = clip_of(sumsq, max_norm);
@@ -181,10 +201,8 @@ __global__ __launch_bounds__(kNormThreads) void tlc_clip_kernel(
     put_result(result, c);
   }
   if (!c.finite || (kOwn && c.coef == 1.0f)) return;
-  const uint32_t p0 = (uint32_t)((uint64_t)blockIdx.x * list.n / gridDim.x);
-  const uint32_t p1 = (uint32_t)((uint64_t)(blockIdx.x + 1) * list.n / gridDim.x);
   for (uint32_t i = p0; i < p1; ++i) {
-    Piece p = piece_of(list, i);
+    if (i > p0) p = piece_of(list, i);
     if (p.type == TLC_F32)
       piece_scale<float, float>(p, c.coef);
     else if (p.type == TLC_BF16)

@@ -37,11 +37,11 @@ constexpr uint32_t kDigitBits = 9;
 constexpr uint32_t kDigits = 1u << kDigitBits;
 constexpr uint32_t kSortThreads = 512;
 constexpr uint32_t kSortTile = kSortThreads * 2;  // the smallest
-constexpr uint32_t kSmallThreads = 1024;
+constexpr uint32_t kSmallThreads = 512;
 // (One launch | sorted first: 1000 tokens of 512 bf16 values added, common ids
-// 9.9 | 22.5 us, three ids in all 17.0 | 22.2; 2000 14.5 | 25.4 and 27.8 | 24.1;
-// 4000 26.9 | 27.5 and 54.0 | 26.7.)
-constexpr uint32_t kSmallTokens = kSmallThreads * 2;
+// 8.4 | 20.9 us; 2000 13.1 | 21.5, three ids in all 19.9 | 21.3; with twice as many
+// the wave that has a common id to itself takes longer than the sort.)
+constexpr uint32_t kSmallTokens = kSmallThreads * 4;
 constexpr uint32_t kSortPasses = 4;  // at most, of 31 bits
 // Up to kNextTiles tiles a pass counts the next one's digits, which saves that
 // pass's count (16000 tokens 28.2 | 29.9 us; 28 tiles, whose counters hold up the
@@ -77,6 +77,11 @@ struct FillArgs {
   Divider group, stride;
 };
 constexpr uint32_t kFillBlocks = 1u << 20;  // of a launch
+// Above so many values to set, few tokens are sorted first too: the sort is over
+// before the zeroes are written, which tiles do faster than blocks that look at
+// all ids (one launch | sorted first, 1000 tokens: 41 MB 12.9 | 24.4 us, 102 MB
+// 23.6 | 32.0, 205 MB 44 | 45, 410 MB 85 | 75, 1065 MB 225 | 174).
+constexpr uint64_t kSmallFillValues = 50000000;
 constexpr uint32_t kSmallFillBlocks = 1024;
 constexpr uint32_t kSmallFillRows = 8192;   // of a block
 // The sums: kSumWaves waves of a block, each per_wave sorted tokens.

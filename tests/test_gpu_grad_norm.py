@@ -220,6 +220,31 @@ def test_other_stream():
         assert near(r.norm, math.sqrt(sumsq_of(ts)), ROUND)
 
 
+def test_thousands_of_tensors():
+    """More tensors than blocks: a block takes several pieces."""
+    sizes = [(53 * i) % 700 + 1 for i in range(5000)]
+    with T().TrainContext(max_tensors=5000) as c:
+        flat = tensors_of(9, [sum(sizes)], ("f32",), 0.1)[0]
+        ts = list(torch.split(flat, sizes))
+        half = flat.bfloat16()
+        mixed = [h if i % 3 else t for i, (t, h) in enumerate(zip(ts, torch.split(half, sizes)))]
+        want = sumsq_of([torch.cat([m.float() for m in mixed])])
+        r = c.grad_norm(mixed)
+        c.sync()
+        assert near(r.sumsq, want, 2.0 ** -40) and near(r.norm, math.sqrt(want), ROUND)
+        out = torch.empty_like(flat)
+        r = c.clip_grad_norm(mixed, 0.3 * math.sqrt(want), outs=list(torch.split(out, sizes)))
+        c.sync()
+        assert bits_equal(out, torch.cat([r.coef * m.float() for m in mixed]))
+        before = flat.clone()
+        for k in range(11):  # more calls than staging slots, without a wait
+            r = c.clip_grad_norm(ts, 1e-3 * 0.5 ** k)
+        c.sync()
+        assert near(r.norm, 1e-3 * 0.5 ** 9, 1e-4)
+        assert torch.allclose(flat, before * (1e-3 * 0.5 ** 10 / float(before.double().norm())),
+                              rtol=1e-4, atol=0.0)
+
+
 def test_capture():
     """A captured norm and clip follow their tensors' new values, with eager
     calls between the replays; longer lists refuse to be captured."""
