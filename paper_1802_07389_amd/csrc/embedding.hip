@@ -1,8 +1,8 @@
 // embedding.hip -- the lookup of embedding rows with scaling:
 //   out[t, :] = round(scale * table[ids[t], :])
 // What bounds it: the rows read (common ones from the caches) and out written
-// once.  65536 tokens of 2048 bf16 values from 131072 rows take 77 us (268 MB
-// written, about 88 MB of distinct rows: 4.6 TB/s, a large copy's rate), a few
+// once.  65536 tokens of 2048 bf16 values from 131072 rows take 75 us (268 MB
+// written, about 88 MB of distinct rows: 4.8 TB/s, a large copy's rate), a few
 // tokens one launch.
 #include "device_common.hpp"
 #include "train_internal.h"
@@ -21,10 +21,12 @@ __device__ __forceinline__ int64_t token_row(const void* ids, uint32_t t, uint32
 }  // namespace
 
 // One pass over the output in packs of V values, kUnits of a thread 256 packs
-// apart (a block per token, value by value: 194 instead of 77 us; eight packs a
-// thread: 80): the ids of all of them are asked for first, then their rows, then
-// the products stored.  A row that is no whole number of packs ends with a pack
-// moved back to end with it (its values are written twice, alike).
+// apart: the ids of all of them are asked for first, then their rows, then the
+// products stored, streaming, so that rows asked for again keep the caches (65536
+// tokens of 1024 fp32 values: 78 us, without the hint 89; of 2048 bf16 values with
+// one pack a thread 82, two 75, four 77, eight 80; a block per token, value by
+// value, 194).  A row that is no whole number of packs ends with a pack moved back
+// to end with it (its values are written twice, alike).
 template <class In, class Id, class Out, int V, int kUnits>
 __global__ __launch_bounds__(kEmbThreads) void tlc_embedding_kernel(EmbArgs a, Divider packs,
                                                                     uint32_t slice) {
@@ -52,7 +54,7 @@ __global__ __launch_bounds__(kEmbThreads) void tlc_embedding_kernel(EmbArgs a, D
     Pack<Out, V> o;
 #pragma unroll
     for (int e = 0; e < V; ++e) o.set(e, row[i] < 0 ? 0.0f : a.scale * x[i].get(e));
-    store_pack<Out, V>(static_cast<Out*>(a.out) + t[i] * a.out_stride + k[i], o);
+    store_pack<Out, V, true>(static_cast<Out*>(a.out) + t[i] * a.out_stride + k[i], o);
     if (row[i] < 0 && k[i] == 0) host_put(a.bad, 1u);
   }
 }
@@ -65,8 +67,8 @@ hipError_t embedding_packs(const EmbArgs& a, hipStream_t st) {
   const uint32_t slice = std::min(a.count, (uint32_t)((1u << 31) - 1) / packs);
   const uint32_t slices = (a.count + slice - 1) / slice;
   const uint32_t units = slice * packs;
-  constexpr int kUnits = 4;
-  // A call that four packs a thread leave without a block for every CU takes
+  constexpr int kUnits = 2;
+  // A call that two packs a thread leave without a block for every CU takes
   // one each.
   if ((units + kEmbThreads * kUnits - 1) / (kEmbThreads * kUnits) < kCus) {
     launch_k(tlc_embedding_kernel<In, Id, Out, V, 1>,
