@@ -288,7 +288,8 @@ typedef struct tlc_train tlc_train;
  * max_tokens tokens (below 2^31) into tables of up to max_rows rows of up to
  * max_dim values, and for lists of up to max_tensors tensors (at most
  * TLC_MAX_TENSORS).  Any of them may be 0: that call is then refused
- * (tlc_embedding needs none of them). */
+ * (tlc_embedding needs none of them).  Allocates one device workspace of about
+ * (24 + max_dim / 8) * max_tokens + max_rows bytes. */
 int tlc_train_create(tlc_train** ctx, size_t max_tokens, size_t max_rows, size_t max_dim,
                      size_t max_tensors, void* hip_stream);
 

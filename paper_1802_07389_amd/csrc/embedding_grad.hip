@@ -116,7 +116,7 @@ __device__ __forceinline__ uint32_t prefix_waves(uint16_t (*n)[kDigits], uint32_
   return sum;
 }
 
-// Sorts 1024 * kItems keys and their numbers within a block, digit by digit.
+// Sorts kSmallThreads * kItems keys and their numbers within a block, digit by digit.
 template <int kItems>
 __device__ __forceinline__ void sort_block(uint32_t (&key)[kItems], uint32_t passes,
                                            uint16_t (*wave_n)[kDigits], uint32_t* base,
@@ -157,7 +157,8 @@ __device__ __forceinline__ void sort_block(uint32_t (&key)[kItems], uint32_t pas
 
 // The counts of a pass's digits in every tile; the first pass's also makes the
 // keys, and marks the rows that any token touches (touched NULL: not wanted).
-// Clears the tables of the s.clear passes after it.  Blocks from `tiles` on fill rows.
+// Clears the tables of the s.clear passes after it.  Blocks from s.tiles on fill
+// rows.
 template <int kItems>
 __global__ __launch_bounds__(kSortThreads) void tlc_token_count_kernel(
     EmbArgs a, SortArgs s, uint32_t* __restrict__ keys, uint8_t* __restrict__ touched,
@@ -410,10 +411,9 @@ struct WaveRuns {
 }  // namespace
 
 // Few tokens in one launch, without a partial row (512 tokens of 256 fp32 values,
-// 8 MB of rows set: 6.5 us, sorted first 23): every block sorts all of
-// them, and takes the runs that begin in its share of the sorted tokens, its
-// waves an equal part each.  Blocks from s.blocks * s.slabs on look at all ids and
-// fill rows.
+// 8 MB of rows set: 6.5 us): every block sorts all of them, and takes the runs that
+// begin in its share of the sorted tokens, its waves an equal part each.  Blocks
+// from s.blocks * s.slabs on look at all ids and fill rows.
 template <class In, int V, bool kAdd, int kItems>
 __global__ __launch_bounds__(kSmallThreads) void tlc_embedding_grad_small_kernel(
     EmbArgs a, SumArgs s, uint32_t passes, FillArgs f) {
@@ -485,11 +485,10 @@ __global__ __launch_bounds__(kSmallThreads) void tlc_embedding_grad_small_kernel
   if (runs.tail) runs.template finish<kW>(a, lds.heads, head, wid, col);
 }
 
-// Every wave: `per_wave` sorted tokens of one slab of columns, whose rows it asks
-// for eight at a time.  Bounded by the rows' bytes, read and written at 5 TB/s
-// together where there are many.  What the block
-// adds to a run that began earlier is its head, what it has of one that goes
-// on its tail: partial rows for the join.
+// Every wave: `per_wave` sorted tokens of one slab of columns.  What the block adds
+// to a run that began earlier is its head, what it has of one that goes on its
+// tail: partial rows for the join.  Bounded by the rows' bytes, read and written at
+// 5.2 TB/s together (131072 tokens of 2048 bf16 values: 825 MB in 156 us).
 template <class In, int V, bool kAdd>
 __global__ __launch_bounds__(kSumThreads) void tlc_embedding_grad_sum_kernel(EmbArgs a,
                                                                              SumArgs s) {
