@@ -3,6 +3,7 @@
 #include <math.h>
 
 #include <new>
+#include <type_traits>
 #include <vector>
 
 #include "api_common.hpp"
@@ -41,6 +42,7 @@ struct tlc_train {
   // device workspace (one allocation)
   void* ws = nullptr;
   double* partials = nullptr;
+  Piece* pieces = nullptr;  // a long list's, for its clipping
   GradWork grad = {};
   // pinned: the sticky index flag and the staging slots of the pieces
   uint32_t* bad = nullptr;
@@ -173,8 +175,9 @@ ArgList arg_list(const ListCall& l) {
   return r;
 }
 
-PinnedList pinned_list(const ListCall& l, Piece* host, const Piece* dev) {
+PinnedList pinned_list(const ListCall& l, Piece* host, const Piece* dev, Piece* copy) {
   PinnedList r = {};
+  r.copy = copy;
   r.own_type = l.clip && !l.outs;
   r.pieces = dev;
   const size_t len = piece_values(l.total, l.count);
@@ -210,7 +213,7 @@ int run_list(tlc_train* c, const char* fn, ListCall l, F&& run) {
   Piece* host = nullptr;
   const Piece* pieces = nullptr;
   st = take_slot(c, &host, &pieces);
-  if (!st) st = launched(c, run(pinned_list(l, host, pieces)), fn);
+  if (!st) st = launched(c, run(pinned_list(l, host, pieces, l.clip ? c->pieces : nullptr)), fn);
   return st ? st : leave_slot(c);
 }
 
@@ -245,9 +248,11 @@ TLC_API int tlc_train_create(tlc_train** out, size_t max_tokens, size_t max_rows
     return hip_fail(e, "hipGetDevice");
   }
   c->slot_pieces = max_tensors > kArgTensors ? kNormBlocks + max_tensors : 0;
-  // layout: partial sums | sorted tokens, twice | counts of the sort |
+  // layout: partial sums | a long list's pieces | sorted tokens, twice | counts of the sort |
   //         touched rows | partial rows
   size_t off = round_up(kNormBlocks * sizeof(double), 256);
+  const size_t off_pieces = off;
+  off = round_up(off + c->slot_pieces * sizeof(Piece), 256);
   size_t off_sort[4];
   for (size_t& o : off_sort) {
     o = off;
@@ -280,6 +285,7 @@ TLC_API int tlc_train_create(tlc_train** out, size_t max_tokens, size_t max_rows
   *c->bad = 0u;
   uint8_t* base = (uint8_t*)c->ws;
   c->partials = (double*)base;
+  c->pieces = (Piece*)(base + off_pieces);
   for (int i = 0; i < 2; ++i) {
     c->grad.keys[i] = (uint32_t*)(base + off_sort[i]);
     c->grad.pos[i] = (uint32_t*)(base + off_sort[2 + i]);
@@ -442,7 +448,10 @@ TLC_API int tlc_clip_grad_norm(tlc_train* c, size_t count, const void* const* te
                   [&](const auto& list) {
                     const hipError_t e = launch_sumsq(list, false, c->partials, c->stream);
                     if (e != hipSuccess) return e;
-                    return launch_clip(list, c->partials, norm_blocks(list.n), max_norm, result,
+                    auto again = list;
+                    if constexpr (std::is_same_v<decltype(again), PinnedList>)
+                      again.pieces = again.copy;
+                    return launch_clip(again, c->partials, norm_blocks(list.n), max_norm, result,
                                        c->stream);
                   });
 }

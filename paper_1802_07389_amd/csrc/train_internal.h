@@ -146,6 +146,9 @@ struct ListTensor {
 };
 struct PinnedList {
   const Piece* pieces;
+  // device memory where the norm leaves the pieces for the clipping, which then
+  // need not wait for the bus (335 tensors 14.3 -> 13.0 us); NULL: no clipping
+  Piece* copy;
   uint32_t n;     // pieces
   bool own_type;  // clipping: out is of x's type (else fp32)
 };
