@@ -550,15 +550,25 @@ class TensorList:
             if not t.is_contiguous():
                 raise ValueError("every tensor of a list must be contiguous")
         self.count = len(self.tensors)
-        if self.outs is not None:
-            if [o.numel() for o in self.outs] != [t.numel() for t in self.tensors]:
-                raise ValueError("tensors and outs differ in their sizes")
-            self.out_ptrs = _arr(ctypes.c_void_p, [_dev_f32(o, "out") for o in self.outs])
-        else:
-            self.out_ptrs = None
+        self.out_ptrs = None if outs is None else self.lay_out(self.outs)
         self.args = _list_args([t.data_ptr() for t in self.tensors],
                                [_type_of(t, "tensor") for t in self.tensors],
                                [t.numel() for t in self.tensors])
+
+    def lay_out(self, outs):
+        """The argument array of float32 tensors for the list's clipped values."""
+        outs = list(outs)
+        if [o.numel() for o in outs] != [t.numel() for t in self.tensors]:
+            raise ValueError("tensors and outs differ in their sizes")
+        return _arr(ctypes.c_void_p, [_dev_f32(o, "out") for o in outs])
+
+
+def _clip_list(tensors, outs):
+    """(list, output array) of a clipping call: outs, where they are given, come
+    before those that a kept list has."""
+    if not isinstance(tensors, TensorList):
+        tensors, outs = TensorList(tensors, outs), None
+    return tensors, tensors.out_ptrs if outs is None else tensors.lay_out(outs)
 
 
 class NormResult:
@@ -654,19 +664,19 @@ class TrainContext:
 
     def clip(self, tensors, max_norm, result, outs=None):
         """Clip a list by result.sumsq, which grad_norm (and a sum over ranks)
-        left there."""
-        ls = tensors if isinstance(tensors, TensorList) else TensorList(tensors, outs)
-        _check(lib.tlc_clip(self.handle, ls.count, *ls.args, max_norm, result.ptr, ls.out_ptrs))
+        left there: into outs, or a kept list's, or in place."""
+        ls, out_ptrs = _clip_list(tensors, outs)
+        _check(lib.tlc_clip(self.handle, ls.count, *ls.args, max_norm, result.ptr, out_ptrs))
         return result
 
     def clip_grad_norm(self, tensors, max_norm, outs=None, result=None):
-        """Clip a list by its global norm (asynchronous): into outs, or in
-        place.  The result's status is TLC_E_NONFINITE, and nothing written,
-        where a value is NaN or Inf."""
-        ls = tensors if isinstance(tensors, TensorList) else TensorList(tensors, outs)
+        """Clip a list by its global norm (asynchronous): into outs, or a kept
+        list's, or in place.  The result's status is TLC_E_NONFINITE, and
+        nothing written, where a value is NaN or Inf."""
+        ls, out_ptrs = _clip_list(tensors, outs)
         r = self.norm_result() if result is None else result
         _check(lib.tlc_clip_grad_norm(self.handle, ls.count, *ls.args, max_norm, r.ptr,
-                                      ls.out_ptrs))
+                                      out_ptrs))
         return r
 
     def sync(self):
