@@ -15,7 +15,10 @@
 
 namespace tlc {
 
+// Also takes the error off the calling thread, where hipGetLastError() after
+// the next launch, of any context or library, would find it again.
 inline int hip_fail(hipError_t e, const char* what) {
+  (void)hipGetLastError();
   return fail(TLC_E_DEVICE, "%s: %s", what, hipGetErrorString(e));
 }
 
