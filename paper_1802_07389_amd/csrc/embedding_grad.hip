@@ -192,6 +192,36 @@ __global__ __launch_bounds__(kSortThreads) void tlc_token_count_kernel(
   }
 }
 
+// Turns the counts of many tiles into their exclusive prefixes over the tiles, and
+// leaves the digits' totals: a block takes kScanDigits digits, its threads equal
+// ranges of tiles, twice.
+__global__ __launch_bounds__(kScanThreads) void tlc_token_scan_kernel(SortArgs s) {
+  constexpr uint32_t kRanges = kScanThreads / kScanDigits;
+  __shared__ uint32_t sums[kRanges][kScanDigits];
+  const uint32_t col = threadIdx.x % kScanDigits, range = threadIdx.x / kScanDigits;
+  const uint32_t digit = blockIdx.x * kScanDigits + col;
+  const uint32_t t0 = (uint32_t)((uint64_t)range * s.tiles / kRanges);
+  const uint32_t t1 = (uint32_t)((uint64_t)(range + 1) * s.tiles / kRanges);
+  uint32_t sum = 0;
+#pragma unroll 8
+  for (uint32_t t = t0; t < t1; ++t) sum += s.counts[t * kDigits + digit];
+  sums[range][col] = sum;
+  __syncthreads();
+  uint32_t before = 0, total = 0;
+#pragma unroll
+  for (uint32_t r = 0; r < kRanges; ++r) {
+    before += r < range ? sums[r][col] : 0u;
+    total += sums[r][col];
+  }
+  if (range == 0) s.totals[digit] = total;
+#pragma unroll 8
+  for (uint32_t t = t0; t < t1; ++t) {
+    const uint32_t n = s.counts[t * kDigits + digit];
+    s.counts[t * kDigits + digit] = before;
+    before += n;
+  }
+}
+
 // One pass over tiles: a tile's keys go where the counts of all tiles send them,
 // those of equal digits in their order.  kNext: also counts the next pass's
 // digits in the tiles that the keys go to (at most kNextTiles), first in LDS:
@@ -224,11 +254,16 @@ __global__ __launch_bounds__(kSortThreads) void tlc_token_sort_kernel(SortArgs s
     for (uint32_t i = threadIdx.x; i < s.tiles * kDigits; i += kSortThreads) next[i] = 0u;
   // the digit's keys in the tiles before this one, and in all
   uint32_t before = 0, total = 0;
+  if (s.totals) {
+    before = s.counts[blockIdx.x * kDigits + threadIdx.x];
+    total = s.totals[threadIdx.x];
+  } else {
 #pragma unroll 16
-  for (uint32_t t = 0; t < s.tiles; ++t) {
-    const uint32_t v = s.counts[t * kDigits + threadIdx.x];
-    before += t < blockIdx.x ? v : 0u;
-    total += v;
+    for (uint32_t t = 0; t < s.tiles; ++t) {
+      const uint32_t v = s.counts[t * kDigits + threadIdx.x];
+      before += t < blockIdx.x ? v : 0u;
+      total += v;
+    }
   }
   __syncthreads();
   rank_keys<kItems>(key, items, s.shift, wave_n[wid], rank);
@@ -605,6 +640,9 @@ int sort_tokens(const EmbArgs& a, const GradWork& w, uint32_t passes, FillArgs f
   s.tiles = (a.count + kTile - 1) / kTile;
   uint8_t* touched = f.tiles ? w.touched : nullptr;
   const bool next = s.tiles <= kNextTiles;  // a pass counts for the one after it
+  // behind the one table of counts, where kSortPasses have room
+  static_assert(kScanTiles >= kNextTiles, "one table");
+  s.totals = s.tiles > kScanTiles ? w.counts + s.tiles * kDigits : nullptr;
   uint32_t launches = next ? passes : 2 * passes - 1;  // that take a share of the fill
   for (uint32_t p = 0; p < passes; ++p) {
     s.keys_in = w.keys[p & 1];
@@ -621,6 +659,8 @@ int sort_tokens(const EmbArgs& a, const GradWork& w, uint32_t passes, FillArgs f
       launch_k(tlc_token_count_kernel<kItems>, s.tiles + fill, kSortThreads, st, a, s, w.keys[0],
                touched, f);
     }
+    if (s.totals)
+      launch_k(tlc_token_scan_kernel, kDigits / kScanDigits, kScanThreads, st, s);
     const uint32_t fill = take_fill(&f, launches--);
     if (s.next)
       launch_k(tlc_token_sort_kernel<kItems, true>, s.tiles + fill, kSortThreads, st, s, f);
@@ -682,9 +722,8 @@ void launch_grad(const EmbArgs& a, const GradWork& w, hipStream_t st) {
                passes, f);
     return;
   }
-  const int at = a.count >= kTile16Tokens  ? sort_tokens<16>(a, w, passes, f, st)
-                 : a.count >= kTile4Tokens ? sort_tokens<4>(a, w, passes, f, st)
-                                           : sort_tokens<2>(a, w, passes, f, st);
+  const int at = a.count >= kTile4Tokens ? sort_tokens<4>(a, w, passes, f, st)
+                                         : sort_tokens<2>(a, w, passes, f, st);
   s.keys = w.keys[at];
   s.pos = w.pos[at];
   s.per_wave = sum_per_wave(a.count, s.slabs);

@@ -29,33 +29,44 @@ hipError_t launch_embedding(const EmbArgs& a, int table_type, int ids_type, int 
 // The gradient's sort by digits of the tokens' rows (heights below 2^18 in two
 // passes).  Up to kSmallTokens tokens every block of the sums sorts them in LDS;
 // more are sorted first, in tiles of two tokens a thread, from kTile4Tokens on of
-// four and from kTile16Tokens on of sixteen: small tiles fill the chip, but every
-// tile's block reads the counts of all (two | four | sixteen a thread: 30000
-// tokens 43.4 | 45.1 | 62.7 us, 130000 52.7 | 47.8 | 66.2, 500000 125 | 100 | 120,
-// 2000000 781 | 385 | 272).
+// four: small tiles fill the chip, but every tile's block reads the counts of all,
+// or all have to be scanned (two | four a thread, 8 fp32 values a token added:
+// 30000 tokens 33 | 35 us, 65536 34 | 36, 130000 52 | 47, 500000 94 | 94, 2000000
+// 252 | 249; of one value 2^24 1.70 | 1.56 ms, 2^27 13.7 | 12.5; sixteen a thread 50
+// us for 30000, 0.26 ms for 2000000, 11.7 ms for 2^27).
 constexpr uint32_t kDigitBits = 9;
 constexpr uint32_t kDigits = 1u << kDigitBits;
 constexpr uint32_t kSortThreads = 512;
 constexpr uint32_t kSortTile = kSortThreads * 2;  // the smallest
 constexpr uint32_t kSmallThreads = 512;
-// (One launch | sorted first: 1000 tokens of 512 bf16 values added, common ids
-// 8.4 | 20.9 us; 2000 13.1 | 21.5, three ids in all 19.9 | 21.3; with twice as many
-// the wave that has a common id to itself takes longer than the sort.)
+// (One launch | sorted first, 512 bf16 values a token added: 1000 tokens of common
+// ids 8.6 | 18.0 us, of three ids in all 12.9 | 17.6; 2000 tokens 13.2 | 19.3 and
+// 19.9 | 18.5.  The host does not know the ids; with twice as many tokens the wave
+// that has a common id to itself takes longer than the sort.)
 constexpr uint32_t kSmallTokens = kSmallThreads * 4;
 constexpr uint32_t kSortPasses = 4;  // at most, of 31 bits
 // Up to kNextTiles tiles a pass counts the next one's digits, which saves that
-// pass's count (16000 tokens 28.2 | 29.9 us; 28 tiles, whose counters hold up the
-// blocks that fill beside, 16384 tokens 68.6 instead of 62.9).
+// pass's count (10000 tokens 30 | 33 us).  Its counters are in LDS, which leaves
+// fewer blocks a CU to fill beside: with room for 28 tiles 16384 tokens of 1024
+// values, 65536 rows set, take 67 instead of 62 us.
 constexpr uint32_t kNextTiles = 16;
 constexpr uint32_t kXcds = 8;
 constexpr uint32_t kTile4Tokens = 1u << 16;
-constexpr uint32_t kTile16Tokens = 1u << 20;
+// Above kScanTiles tiles a launch of its own turns a pass's counts into their
+// prefixes, so that what the blocks read does not grow with the square of the
+// tiles (every block reading all counts | prefixes, two passes over tokens of one
+// value: 200000 tokens, 98 tiles, 52 | 54 us; 500000 88 | 83; in tiles of sixteen a
+// thread, 2^20 tokens 145 | 145, 2^21 244 | 235, 2^24 2.15 | 1.54 ms, 2^27 102 | 11.7).
+constexpr uint32_t kScanTiles = 128;
+constexpr uint32_t kScanDigits = 16;  // of a block: 64 bytes of every tile's counts
+constexpr uint32_t kScanThreads = 512;
 struct SortArgs {
   const uint32_t* keys_in;
   const uint32_t* pos_in;  // NULL: the tokens in their order
   uint32_t* keys_out;
   uint32_t* pos_out;
   uint32_t* counts;  // per tile and digit
+  uint32_t* totals;  // per digit; counts then hold prefixes.  NULL: they are counts
   uint32_t* next;    // the next pass's, or NULL
   uint32_t count, tiles, shift;
   uint32_t clear;    // tables to clear behind counts
