@@ -398,7 +398,8 @@ class Context:
         _check(tlc_ctx_set_options(self.handle, options))
 
     def close(self):
-        if getattr(self, "handle", None):
+        # at the interpreter's exit this module's names may be gone before the context
+        if getattr(self, "handle", None) and tlc_ctx_destroy is not None:
             tlc_ctx_destroy(self.handle)
             self.handle = None
 
@@ -598,7 +599,8 @@ class TrainContext:
                                            int(max_tensors), self.stream.cuda_stream)
 
     def close(self):
-        if getattr(self, "handle", None):
+        # at the interpreter's exit this module's names may be gone before the context
+        if getattr(self, "handle", None) and tlc_train_destroy is not None:
             tlc_train_destroy(self.handle)
             self.handle = None
 
