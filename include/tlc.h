@@ -268,7 +268,10 @@ int tlc_compress_noalloc(const float* tensor, float* residual, size_t n, float s
  * device memory owned by the caller, the same rules for host threads and
  * errors.  Their calls may be captured into a graph (lists of tensors: up to
  * TLC_CAPTURE_TENSORS; longer ones are handed over in host memory that later
- * calls use again, and refused).  tlc_profile_* does not time them. */
+ * calls use again, and refused).  A replay uses the context's workspace like the
+ * calls that it holds: it runs on the context's stream or is ordered with the
+ * context's other work by the caller, and before tlc_train_destroy().
+ * tlc_profile_* does not time them. */
 typedef struct tlc_train tlc_train;
 
 #define TLC_CAPTURE_TENSORS 128
@@ -347,8 +350,11 @@ typedef struct tlc_norm_result {
 /* The global norm of `count` tensors: result->sumsq, norm and status (coef is
  * 1).  Host arrays of device pointers, of types and of value counts (each at
  * most TLC_MAX_N, 2^40 in all); a tensor of no values may be NULL.  Squares and sums are
- * in 64 bits: no value of any type overflows them, and the order of the sums,
- * fixed by the sizes, is not seen in the norm. */
+ * in 64 bits: no value of any type overflows them.  The order of the sums is fixed by
+ * the sizes: the same call gives the same bits.  The same values cut into other
+ * tensors are added in another order, which can change the last bits of sumsq and,
+ * where its root lies that close between two fp32 values, norm by one unit in the
+ * last place. */
 int tlc_grad_norm(tlc_train* ctx, size_t count, const void* const* tensors, const int* types,
                   const size_t* ns, tlc_norm_result* result);
 

@@ -25,8 +25,9 @@ __device__ __forceinline__ int64_t token_row(const void* ids, uint32_t t, uint32
 // products stored, streaming, so that rows asked for again keep the caches (65536
 // tokens of 1024 fp32 values: 78 us, without the hint 89; of 2048 bf16 values with
 // one pack a thread 82, two 75, four 77, eight 80; a block per token, value by
-// value, 194).  A row that is no whole number of packs ends with a pack moved back
-// to end with it (its values are written twice, alike).
+// value, 194; 2 to 32 MB looked up and read by the next kernel take the same with
+// and without the hint).  A row that is no whole number of packs ends with a pack
+// moved back to end with it (its values are written twice, alike).
 template <class In, class Id, class Out, int V, int kUnits>
 __global__ __launch_bounds__(kEmbThreads) void tlc_embedding_kernel(EmbArgs a, Divider packs,
                                                                     uint32_t slice) {

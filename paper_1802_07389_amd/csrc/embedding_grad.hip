@@ -16,8 +16,11 @@
 // 131072 tokens of 2048 bf16 values into 131072 rows (537 MB read, 1.07 GB
 // written): 295 us, 5.5 TB/s, of which the sums and their rows 155, the zeroes and
 // the sort beside them 130.  16384 tokens of 1024 values into 65536 rows: 61 us.
-// 10007 tokens of 515 fp16 values added to what is there: 29 us, five launches one
-// after the other, most of it their latency.
+// 10007 tokens of 515 fp16 values added to what is there: 29 us, five dependent
+// launches of 3.5 to 9 us (of a few blocks: 2).  Little of that is bytes: each is a
+// chain of dependent loads, ballots and barriers, the sort's in ten blocks.
+// The stores are hinted (streaming); a gradient of 8, 64 or 256 MB and its encode
+// take the same with and without that.
 #include "device_common.hpp"
 #include "train_internal.h"
 #include "typed_io.hpp"

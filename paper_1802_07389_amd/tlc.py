@@ -587,7 +587,11 @@ class TrainContext:
     """The training-step operators around the codec, on one stream: embedding
     lookups and gradients, the gradient norm and clipping.  Work is ordered on
     that stream (by default torch's current one when the context is made):
-    tensors that another stream makes or uses are waited for by the caller."""
+    tensors that another stream makes or uses, and replays of captured calls on
+    another stream, are waited for by the caller.  The calls are not part of
+    torch's autograd: results have no grad_fn, also where a table requires
+    gradients, and what is written in place does not count in a tensor's
+    version.  A program calls embedding_grad() in its backward pass."""
 
     def __init__(self, max_tokens=0, max_rows=0, max_dim=0, max_tensors=0, stream=None,
                  device=None):
