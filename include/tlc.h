@@ -56,7 +56,7 @@ extern "C" {
 #define TLC_E_NONFINITE (-3) /* NaN/Inf in tensor+residual, or max*s overflows */
 #define TLC_E_CORRUPT (-4)   /* compressed stream does not expand to ceil(n/5) bytes */
 #define TLC_E_DEVICE (-5)    /* HIP runtime error, or the context is unusable */
-#define TLC_E_INDEX (-6)     /* a token id outside the embedding table */
+#define TLC_E_INDEX (-6)     /* a token id outside the embedding table or the vocabulary */
 
 /* Largest number of values one call accepts, summed over a batch (the
  * quartic byte counts must fit the 30-bit counters of the zero-run scans). */
@@ -268,9 +268,10 @@ int tlc_compress_noalloc(const float* tensor, float* residual, size_t n, float s
  * device memory owned by the caller, the same rules for host threads and
  * errors.  Their calls may be captured into a graph (lists of tensors: up to
  * TLC_CAPTURE_TENSORS; longer ones are handed over in host memory that later
- * calls use again, and refused).  A replay uses the context's workspace like the
- * calls that it holds: it runs on the context's stream or is ordered with the
- * context's other work by the caller, and before tlc_train_destroy().
+ * calls use again, and refused; tlc_adamw's of any length).  A replay uses the
+ * context's workspace like the calls that it holds: it runs on the context's
+ * stream or is ordered with the context's other work by the caller, and before
+ * tlc_train_destroy().
  * tlc_profile_* does not time them. */
 typedef struct tlc_train tlc_train;
 
@@ -292,7 +293,7 @@ typedef struct tlc_train tlc_train;
  * max_dim values, and for lists of up to max_tensors tensors (at most
  * TLC_MAX_TENSORS).  Any of them may be 0: that call is then refused
  * (tlc_embedding needs none of them).  Allocates one device workspace of about
- * (24 + max_dim / 8) * max_tokens + max_rows bytes. */
+ * 1.1 MB + (24 + max_dim / 8) * max_tokens + max_rows bytes. */
 int tlc_train_create(tlc_train** ctx, size_t max_tokens, size_t max_rows, size_t max_dim,
                      size_t max_tensors, void* hip_stream);
 
@@ -300,7 +301,8 @@ int tlc_train_create(tlc_train** ctx, size_t max_tokens, size_t max_rows, size_t
 int tlc_train_destroy(tlc_train* ctx);
 
 /* Wait for all work of the context and return (then clear) the sticky
- * status of its lookups and embedding gradients: TLC_OK or TLC_E_INDEX. */
+ * status of its lookups, embedding gradients and token log probabilities: TLC_OK or
+ * TLC_E_INDEX. */
 int tlc_train_sync(tlc_train* ctx);
 
 /* Embedding lookup with scaling: for every token t
@@ -378,6 +380,138 @@ int tlc_clip(tlc_train* ctx, size_t count, const void* const* tensors, const int
 int tlc_clip_grad_norm(tlc_train* ctx, size_t count, const void* const* tensors,
                        const int* types, const size_t* ns, float max_norm,
                        tlc_norm_result* result, float* const* outs);
+
+/* ---- the loss, and the server's step --------------------------------------
+ *
+ * The ends of the same training step, on the same contexts: the log
+ * probabilities of given tokens (their negative mean is a language model's
+ * loss) with their gradient, and the optimizer's step that turns the gradients
+ * which tlc_decompress_sum has added up into new weights and into the change
+ * that tlc_compress encodes for the workers' pulls. */
+
+/* Most alternatives of a token, and the values that share a scale of the
+ * optimizer's states in 8 bits. */
+#define TLC_MAX_TOP 64
+#define TLC_STATE_BLOCK 256
+
+/* Of one row of logits x with scale s, in device memory. */
+typedef struct tlc_token_result {
+  float logprob; /* s * (x[target] - max) - log_sum; 0 without a target */
+  float entropy; /* -sum p ln p, p = exp(s * (x - max) - log_sum) */
+  float max;     /* the largest logit, as it is in the row */
+  float log_sum; /* ln sum exp(s * (x - max)) */
+} tlc_token_result;
+
+/* Log probabilities of given tokens, the entropy of every row and its most
+ * likely alternatives, from logits that are read once.
+ *   logits        device, count rows of vocab values of type (vocab in [1,
+ *                 TLC_MAX_DIM], count below 2^31), stride values apart (any).
+ *   scale         of the logits, in (0, 1e18]: the inverse temperature.
+ *   targets       device int32 or int64 [count] (ids_type), or NULL: none.
+ *   ignore_id     rows with this target (any value) are left out: not read,
+ *                 all their outputs 0 and their top_ids -1.  So are rows
+ *                 whose target is outside [0, vocab); the next
+ *                 tlc_train_sync() then returns TLC_E_INDEX.
+ *   results       device [count].
+ *   top           alternatives of a row, at most TLC_MAX_TOP and vocab:
+ *                 top_logprobs and top_ids (device, count rows of top, NULL
+ *                 for none) hold the largest logits' log probabilities and
+ *                 columns, the largest first, the lowest column first among
+ *                 equal logits.
+ * Sums are in fp32 in an order that the sizes alone fix.  Entries of -inf have
+ * probability 0.  A row with no other entry has max, log_sum and log probabilities -inf
+ * and entropy 0; its top_ids are its first columns.  A row that holds NaN or
+ * +inf has NaN in its place, and top_ids -1.  No output may overlap another
+ * argument. */
+int tlc_token_logprobs(tlc_train* ctx, const void* logits, int type, size_t count, size_t vocab,
+                       size_t stride, float scale, const void* targets, int ids_type,
+                       int64_t ignore_id, tlc_token_result* results, size_t top,
+                       float* top_logprobs, int32_t* top_ids);
+
+/* The gradient of logits from those of the log probabilities and entropies
+ * that tlc_token_logprobs gave:
+ *   out[t, j] = round(scale * (a (1[j = target] - p_j) - b p_j (ln p_j + entropy)))
+ * with a = grad_logprob[t] and b = grad_entropy[t] (device fp32 [count]; NULL:
+ * zeroes) and p from results.  Rows that are left out (see there) and rows of
+ * -inf alone get zeroes and are not read; a row of NaN gets NaN.
+ *   out           device, count rows of vocab values of out_type, out_stride >=
+ *                 vocab values apart; values between rows are left alone.
+ *                 It may be logits itself (the same address, type and
+ *                 stride); apart from that it must not overlap another argument.
+ * Without targets grad_logprob must be NULL. */
+int tlc_token_logprobs_grad(tlc_train* ctx, const void* logits, int type, size_t count,
+                            size_t vocab, size_t stride, float scale, const void* targets,
+                            int ids_type, int64_t ignore_id, const tlc_token_result* results,
+                            const float* grad_logprob, const float* grad_entropy, void* out,
+                            int out_type, size_t out_stride);
+
+/* How an optimizer's states are held. */
+#define TLC_STATE_F32 0
+#define TLC_STATE_8BIT 1
+
+/* Steps done, in device memory: {0, 1.0f, 0} before the first one. */
+typedef struct tlc_adamw_clock {
+  int64_t step;      /* of steps done; tlc_adamw counts it up */
+  float lr_scale;    /* factor of lr: a schedule that a graph's replays follow */
+  uint32_t reserved; /* 0 */
+} tlc_adamw_clock;
+
+typedef struct tlc_adamw_options {
+  double lr;           /* finite, >= 0 */
+  double beta1, beta2; /* in [0, 1) */
+  double eps;          /* finite, above 0 in fp32 */
+  double weight_decay; /* finite, >= 0 */
+  float max_norm;      /* >= 0, may be infinite; read where there is a result */
+} tlc_adamw_options;
+
+/* One step of AdamW over `count` tensors (at most the context's max_tensors).
+ * With t = clock->step + 1, lr = options->lr * clock->lr_scale and the factors
+ * rounded to fp32 from 64 bits
+ *   c1 = 1 - beta1, c2 = 1 - beta2, d = lr * weight_decay,
+ *   a = lr / (1 - beta1^t),  r = 1 / sqrt(1 - beta2^t),
+ * every value takes, each operation rounded to fp32,
+ *   g = coef * grad
+ *   m = m + (g - m) * c1
+ *   v = v + (g * g - v) * c2
+ *   new = param - (a * (m / (sqrt(v) * r + eps)) + d * param)
+ * and new is rounded half to even to the parameter's type.
+ *   params, types, grads, grad_types, ns
+ *                 host arrays of device pointers, types and value counts
+ *                 (each at most TLC_MAX_N, 2^40 in all); a tensor of no
+ *                 values may be NULL.
+ *   exp_avgs, exp_avg_sqs
+ *                 the states m and v, device buffers of ns[i] values: fp32,
+ *                 or with state_type TLC_STATE_8BIT bytes (below).  Zeroes
+ *                 before the first step.
+ *   scales        TLC_STATE_8BIT: device buffers of two floats (of m and of v)
+ *                 for every TLC_STATE_BLOCK values; else NULL.
+ *   deltas        NULL, or device fp32 buffers that get new - param, as stored
+ *                 and rounded once; deltas[i] may be grads[i] itself where
+ *                 that is fp32.
+ *   clock         device; its step becomes t.
+ *   result        NULL: coef is 1.  Else the norm of the gradients as
+ *                 tlc_grad_norm left it: coef and the result's fields are
+ *                 those of tlc_clip with options->max_norm, without the
+ *                 clipped gradients' being written anywhere.  Where sumsq is not
+ *                 finite the step is left out: nothing is written but
+ *                 zeroes in deltas and the result, and the clock stays.
+ * A state in 8 bits is an OCP E4M3 (m) or E5M2 (v) number times its block's
+ * scale: after a step, scale = max(largest |m| * (1 / 448), 2^-126) (v: 1 / 57344;
+ * the constant rounded to fp32), 0 where all are 0.  |m| / scale lies between two
+ * codes (0 being one, the largest 448 or 57344) and goes to the upper one where its
+ * share of the way there plus a dither reaches 1: with
+ *   h = (k * 0xC13FA9A9 + t * 0x91E10DA5) mod 2^32
+ * of value k of its tensor, the top 20 bits of h (m) or the top 21 of h xor
+ * 2^31 (v) as a fraction.  Over steps and neighbours these are spread evenly,
+ * so that a slow mean is followed where rounding to nearest would hold still.
+ * v > 0 never gets the code 0.  A block in which a value of m (v) is NaN or infinite
+ * has the scale NaN.
+ * No buffer may overlap another one that is written. */
+int tlc_adamw(tlc_train* ctx, size_t count, void* const* params, const int* types,
+              const size_t* ns, const void* const* grads, const int* grad_types, int state_type,
+              void* const* exp_avgs, void* const* exp_avg_sqs, float* const* scales,
+              float* const* deltas, const tlc_adamw_options* options, tlc_adamw_clock* clock,
+              tlc_norm_result* result);
 
 /* ---- options ------------------------------------------------------------ */
 

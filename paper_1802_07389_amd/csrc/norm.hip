@@ -38,27 +38,6 @@ __device__ __forceinline__ double sum_partials(const double* partials, uint32_t 
   return block_sum(v, lds);
 }
 
-struct Clip {
-  float norm, coef;
-  bool finite;
-};
-__device__ __forceinline__ Clip clip_of(double sumsq, float max_norm) {
-  const double norm = sqrt(sumsq);
-  Clip c;
-  c.finite = sumsq >= 0.0 && sumsq <= DBL_MAX;  // false for NaN too
-  c.norm = (float)norm;
-  c.coef = !c.finite ? __builtin_nanf("")
-                     : (norm > (double)max_norm ? (float)((double)max_norm / norm) : 1.0f);
-  return c;
-}
-
-__device__ __forceinline__ void put_result(tlc_norm_result* r, Clip c) {
-  r->norm = c.norm;
-  r->coef = c.coef;
-  r->status = c.finite ? TLC_OK : TLC_E_NONFINITE;
-  r->reserved = 0u;
-}
-
 // Piece p of a list.
 __device__ __forceinline__ Piece piece_of(const PinnedList& list, uint32_t p) {
   return list.pieces[p];

@@ -2,6 +2,7 @@
 // argument checks, their context's workspace and the launches on its stream.
 #include <math.h>
 
+#include <initializer_list>
 #include <new>
 #include <type_traits>
 #include <vector>
@@ -19,6 +20,7 @@ namespace {
 // pieces).
 constexpr int kGroups = 2, kGroupSlots = 4;
 constexpr size_t kMaxListValues = (size_t)1 << 40;
+constexpr float kMaxLogitScale = 1e18f;
 
 bool known_type(int type) { return type == TLC_F32 || type == TLC_BF16 || type == TLC_F16; }
 
@@ -54,7 +56,11 @@ struct tlc_train {
   bool group_used[kGroups] = {};
   int slot_next = 0;
   // host tables, reserved at creation so that the calls do not allocate
-  std::vector<Span> spans, spans_ok;
+  std::vector<Span> spans, spans_ok, adamw_ok;
+  // token log probabilities: the parts of cut rows; AdamW: the last launch's ticket
+  LogitPart* logit_part = nullptr;
+  uint64_t* logit_keys = nullptr;
+  uint32_t* ticket = nullptr;
 };
 
 namespace {
@@ -248,9 +254,15 @@ TLC_API int tlc_train_create(tlc_train** out, size_t max_tokens, size_t max_rows
     return hip_fail(e, "hipGetDevice");
   }
   c->slot_pieces = max_tensors > kArgTensors ? kNormBlocks + max_tensors : 0;
-  // layout: partial sums | a long list's pieces | sorted tokens, twice | counts of the sort |
-  //         touched rows | partial rows
+  // layout: partial sums | ticket | logits' parts | their keys | a long list's pieces |
+  //         sorted tokens, twice | counts of the sort | touched rows | partial rows
   size_t off = round_up(kNormBlocks * sizeof(double), 256);
+  const size_t off_ticket = off;
+  off += 256;
+  const size_t off_logit_part = off;
+  off = round_up(off + kLogBlocks * sizeof(LogitPart), 256);
+  const size_t off_logit_keys = off;
+  off = round_up(off + kLogBlocks * TLC_MAX_TOP * sizeof(uint64_t), 256);
   const size_t off_pieces = off;
   off = round_up(off + c->slot_pieces * sizeof(Piece), 256);
   size_t off_sort[4];
@@ -268,6 +280,7 @@ TLC_API int tlc_train_create(tlc_train** out, size_t max_tokens, size_t max_rows
                            sizeof(float), 256);
   e = hipMalloc(&c->ws, off);
   if (e == hipSuccess) e = hipMemset((uint8_t*)c->ws + off_touched, 0, max_rows);
+  if (e == hipSuccess) e = hipMemset((uint8_t*)c->ws + off_ticket, 0, 256);
   if (e == hipSuccess) e = hipDeviceSynchronize();
   if (e == hipSuccess) e = hipHostMalloc((void**)&c->bad, 256, hipHostMallocDefault);
   if (e == hipSuccess) e = hipHostGetDevicePointer((void**)&c->bad_dev, c->bad, 0);
@@ -285,6 +298,9 @@ TLC_API int tlc_train_create(tlc_train** out, size_t max_tokens, size_t max_rows
   *c->bad = 0u;
   uint8_t* base = (uint8_t*)c->ws;
   c->partials = (double*)base;
+  c->ticket = (uint32_t*)(base + off_ticket);
+  c->logit_part = (LogitPart*)(base + off_logit_part);
+  c->logit_keys = (uint64_t*)(base + off_logit_keys);
   c->pieces = (Piece*)(base + off_pieces);
   for (int i = 0; i < 2; ++i) {
     c->grad.keys[i] = (uint32_t*)(base + off_sort[i]);
@@ -294,8 +310,9 @@ TLC_API int tlc_train_create(tlc_train** out, size_t max_tokens, size_t max_rows
   c->grad.touched = base + off_touched;
   c->grad.parts = (float*)(base + off_parts);
   try {
-    c->spans.reserve(2 * max_tensors + 1);
+    c->spans.reserve(6 * max_tensors + 2);
     c->spans_ok.reserve(2 * max_tensors + 1);
+    c->adamw_ok.reserve(6 * max_tensors + 2);
   } catch (...) {
     tlc_train_destroy(c);
     return fail(TLC_E_DEVICE, "tlc_train_create: out of host memory");
@@ -327,7 +344,7 @@ TLC_API int tlc_train_sync(tlc_train* c) {
   volatile uint32_t* bad = c->bad;
   if (*bad) {
     *bad = 0u;
-    return fail(TLC_E_INDEX, "a token id is outside the embedding table");
+    return fail(TLC_E_INDEX, "a token id is outside the embedding table or the vocabulary");
   }
   return TLC_OK;
 }
@@ -416,6 +433,138 @@ TLC_API int tlc_embedding_grad(tlc_train* c, const void* grad, int grad_type, si
                                            c->stream), fn);
 }
 
+// ---------------------------------------------------------------- token log probabilities
+namespace {
+
+// What both calls are given; bytes: of the logits.
+int check_logits(const char* fn, const LogitArgs& a, int type, size_t count, size_t vocab,
+                 int ids_type, size_t* bytes) {
+  if (vocab == 0 || vocab > TLC_MAX_DIM)
+    return fail(TLC_E_INVALID, "%s: vocab = %zu not in [1, %d]", fn, vocab, TLC_MAX_DIM);
+  if (count > INT32_MAX) return fail(TLC_E_INVALID, "%s: %zu rows", fn, count);
+  if (!known_type(type)) return fail(TLC_E_INVALID, "%s: unknown type %d", fn, type);
+  if (a.targets && ids_type != TLC_I32 && ids_type != TLC_I64)
+    return fail(TLC_E_INVALID, "%s: unknown type of targets %d", fn, ids_type);
+  if (!(a.scale > 0.0f && a.scale <= kMaxLogitScale))
+    return fail(TLC_E_INVALID, "%s: scale %g not in (0, %g]", fn, (double)a.scale,
+                (double)kMaxLogitScale);
+  if (count && !a.x) return fail(TLC_E_INVALID, "%s: NULL logits", fn);
+  if (!rows_extent(count, vocab, a.stride, type_bytes(type), bytes))
+    return fail(TLC_E_INVALID, "%s: strides beyond the address space", fn);
+  return TLC_OK;
+}
+
+LogitArgs logit_args(tlc_train* c, const void* logits, size_t count, size_t vocab, size_t stride,
+                     float scale, const void* targets, int ids_type, int64_t ignore_id) {
+  LogitArgs a = {};
+  a.x = logits;
+  a.stride = stride;
+  a.count = (uint32_t)count;
+  a.vocab = (uint32_t)vocab;
+  a.scale = scale;
+  a.targets = targets;
+  a.wide_ids = ids_type == TLC_I64;
+  a.ignore = ignore_id;
+  a.bad = c->bad_dev;
+  return a;
+}
+
+size_t id_bytes(int ids_type) { return ids_type == TLC_I64 ? 8 : 4; }
+
+// Of a few spans: without a table of the context's.
+bool few_conflict(std::initializer_list<Span> spans) {
+  for (const Span& a : spans)
+    for (const Span& b : spans)
+      if (&a != &b && a.written && a.lo < b.hi && b.lo < a.hi) return true;
+  return false;
+}
+
+Span span_of(const void* p, size_t bytes, bool written) {
+  return Span{(uintptr_t)p, (uintptr_t)p + (p ? bytes : 0), written};
+}
+
+}  // namespace
+
+TLC_API int tlc_token_logprobs(tlc_train* c, const void* logits, int type, size_t count,
+                               size_t vocab, size_t stride, float scale, const void* targets,
+                               int ids_type, int64_t ignore_id, tlc_token_result* results,
+                               size_t top, float* top_logprobs, int32_t* top_ids) {
+  const char* fn = "tlc_token_logprobs";
+  int st = check_usable(c, fn);
+  if (st) return st;
+  TokenArgs a = {};
+  static_cast<LogitArgs&>(a) =
+      logit_args(c, logits, count, vocab, stride, scale, targets, ids_type, ignore_id);
+  size_t bytes = 0;
+  st = check_logits(fn, a, type, count, vocab, ids_type, &bytes);
+  if (st) return st;
+  if (top > TLC_MAX_TOP || top > vocab)
+    return fail(TLC_E_INVALID, "%s: %zu alternatives of %zu columns (%d at most)", fn, top, vocab,
+                TLC_MAX_TOP);
+  if (count == 0) return TLC_OK;
+  if (!results || (top && (!top_logprobs || !top_ids)))
+    return fail(TLC_E_INVALID, "%s: NULL device pointer", fn);
+  if (few_conflict({span_of(logits, bytes, false),
+                    span_of(targets, count * id_bytes(ids_type), false),
+                    span_of(results, count * sizeof(*results), true),
+                    span_of(top ? top_logprobs : nullptr, count * top * 4, true),
+                    span_of(top ? top_ids : nullptr, count * top * 4, true)}))
+    return fail(TLC_E_INVALID, "%s: an output overlaps another argument", fn);
+  DeviceScope dev(c->device);
+  st = dev.status();
+  if (st) return st;
+  a.results = results;
+  a.top = (uint32_t)top;
+  a.top_logprobs = top_logprobs;
+  a.top_ids = top_ids;
+  a.part = c->logit_part;
+  a.keys = c->logit_keys;
+  return launched(c, launch_token_logprobs(a, type, c->stream), fn);
+}
+
+TLC_API int tlc_token_logprobs_grad(tlc_train* c, const void* logits, int type, size_t count,
+                                    size_t vocab, size_t stride, float scale, const void* targets,
+                                    int ids_type, int64_t ignore_id,
+                                    const tlc_token_result* results, const float* grad_logprob,
+                                    const float* grad_entropy, void* out, int out_type,
+                                    size_t out_stride) {
+  const char* fn = "tlc_token_logprobs_grad";
+  int st = check_usable(c, fn);
+  if (st) return st;
+  TokenGradArgs a = {};
+  static_cast<LogitArgs&>(a) =
+      logit_args(c, logits, count, vocab, stride, scale, targets, ids_type, ignore_id);
+  size_t bytes = 0, out_bytes = 0;
+  st = check_logits(fn, a, type, count, vocab, ids_type, &bytes);
+  if (st) return st;
+  if (!known_type(out_type)) return fail(TLC_E_INVALID, "%s: unknown type %d", fn, out_type);
+  if (grad_logprob && !targets)
+    return fail(TLC_E_INVALID, "%s: a gradient of log probabilities without targets", fn);
+  if (count == 0) return TLC_OK;
+  if (!results || !out) return fail(TLC_E_INVALID, "%s: NULL device pointer", fn);
+  if (out_stride < vocab)
+    return fail(TLC_E_INVALID, "%s: out_stride %zu below vocab %zu", fn, out_stride, vocab);
+  if (!rows_extent(count, vocab, out_stride, type_bytes(out_type), &out_bytes))
+    return fail(TLC_E_INVALID, "%s: strides beyond the address space", fn);
+  const bool in_place =
+      out == logits && out_type == type && (out_stride == stride || count == 1);
+  if (few_conflict({span_of(in_place ? nullptr : logits, bytes, false),
+                    span_of(targets, count * id_bytes(ids_type), false),
+                    span_of(results, count * sizeof(*results), false),
+                    span_of(grad_logprob, count * 4, false),
+                    span_of(grad_entropy, count * 4, false), span_of(out, out_bytes, true)}))
+    return fail(TLC_E_INVALID, "%s: out overlaps another argument", fn);
+  DeviceScope dev(c->device);
+  st = dev.status();
+  if (st) return st;
+  a.results = results;
+  a.grad_logprob = grad_logprob;
+  a.grad_entropy = grad_entropy;
+  a.out = out;
+  a.out_stride = out_stride;
+  return launched(c, launch_token_grad(a, type, out_type, c->stream), fn);
+}
+
 // ---------------------------------------------------------------- norm, clip
 TLC_API int tlc_grad_norm(tlc_train* c, size_t count, const void* const* tensors,
                           const int* types, const size_t* ns, tlc_norm_result* result) {
@@ -454,4 +603,145 @@ TLC_API int tlc_clip_grad_norm(tlc_train* c, size_t count, const void* const* te
                     return launch_clip(again, c->partials, norm_blocks(list.n), max_norm, result,
                                        c->stream);
                   });
+}
+
+// ---------------------------------------------------------------- AdamW
+namespace {
+
+struct AdamCall {
+  size_t count;
+  void* const* params;
+  const int* types;
+  const size_t* ns;
+  const void* const* grads;
+  const int* grad_types;
+  int state_type;
+  void* const* exp_avgs;
+  void* const* exp_avg_sqs;
+  float* const* scales;
+  float* const* deltas;
+  tlc_adamw_clock* clock;
+  tlc_norm_result* result;
+  bool small() const { return state_type == TLC_STATE_8BIT; }
+};
+
+int check_options(const char* fn, const tlc_adamw_options* o, bool clips) {
+  if (!o) return fail(TLC_E_INVALID, "%s: NULL options", fn);
+  if (!(isfinite(o->lr) && o->lr >= 0.0))
+    return fail(TLC_E_INVALID, "%s: lr %g is not finite and >= 0", fn, o->lr);
+  for (double b : {o->beta1, o->beta2})
+    if (!(b >= 0.0 && b < 1.0)) return fail(TLC_E_INVALID, "%s: beta %g not in [0, 1)", fn, b);
+  if (!(isfinite((float)o->eps) && (float)o->eps > 0.0f))
+    return fail(TLC_E_INVALID, "%s: eps %g is not finite and above 0", fn, o->eps);
+  if (!(isfinite(o->weight_decay) && o->weight_decay >= 0.0))
+    return fail(TLC_E_INVALID, "%s: weight_decay %g is not finite and >= 0", fn, o->weight_decay);
+  if (clips && !(o->max_norm >= 0.0f))
+    return fail(TLC_E_INVALID, "%s: max_norm %g is not >= 0", fn, (double)o->max_norm);
+  return TLC_OK;
+}
+
+int check_adamw(tlc_train* c, const char* fn, const AdamCall& l) {
+  if (!l.clock) return fail(TLC_E_INVALID, "%s: NULL clock", fn);
+  if (l.state_type != TLC_STATE_F32 && l.state_type != TLC_STATE_8BIT)
+    return fail(TLC_E_INVALID, "%s: unknown type of states %d", fn, l.state_type);
+  if (l.count && (!l.params || !l.types || !l.ns || !l.grads || !l.grad_types || !l.exp_avgs ||
+                  !l.exp_avg_sqs || (l.small() && !l.scales)))
+    return fail(TLC_E_INVALID, "%s: NULL argument", fn);
+  if (l.count > c->max_tensors)
+    return fail(TLC_E_INVALID, "%s: %zu tensors exceed the context's %zu", fn, l.count,
+                c->max_tensors);
+  c->spans.clear();
+  add_span(c->spans, l.clock, sizeof(*l.clock), true);
+  if (l.result) add_span(c->spans, l.result, sizeof(*l.result), true);
+  size_t total = 0;
+  for (size_t i = 0; i < l.count; ++i) {
+    const size_t n = l.ns[i];
+    if (n == 0) continue;
+    if (!known_type(l.types[i]) || !known_type(l.grad_types[i]))
+      return fail(TLC_E_INVALID, "%s: tensor %zu: unknown type %d or %d", fn, i, l.types[i],
+                  l.grad_types[i]);
+    if (n > TLC_MAX_N)
+      return fail(TLC_E_INVALID, "%s: tensor %zu: n = %zu too large", fn, i, n);
+    if (!l.params[i] || !l.grads[i] || !l.exp_avgs[i] || !l.exp_avg_sqs[i] ||
+        (l.small() && !l.scales[i]) || (l.deltas && !l.deltas[i]))
+      return fail(TLC_E_INVALID, "%s: tensor %zu: NULL pointer", fn, i);
+    total += n;
+    const size_t state = l.small() ? 1 : 4;
+    const bool in_place = l.deltas && (const void*)l.deltas[i] == l.grads[i] &&
+                          l.grad_types[i] == TLC_F32;
+    add_span(c->spans, l.params[i], n * type_bytes(l.types[i]), true);
+    add_span(c->spans, l.grads[i], n * type_bytes(l.grad_types[i]), in_place);
+    add_span(c->spans, l.exp_avgs[i], n * state, true);
+    add_span(c->spans, l.exp_avg_sqs[i], n * state, true);
+    if (l.small()) add_span(c->spans, l.scales[i], ceil_div(n, TLC_STATE_BLOCK) * 8, true);
+    if (l.deltas && !in_place) add_span(c->spans, l.deltas[i], n * 4, true);
+  }
+  if (total > kMaxListValues)
+    return fail(TLC_E_INVALID, "%s: %zu values exceed %zu", fn, total, kMaxListValues);
+  if (spans_conflict_cached(c->spans, c->adamw_ok))
+    return fail(TLC_E_INVALID, "%s: a written buffer overlaps another one", fn);
+  return TLC_OK;
+}
+
+// Tensors [first, next) of the call that have values, kAdamTensors at most.
+AdamList adam_list(const AdamCall& l, size_t first, size_t* next) {
+  AdamList r = {};
+  size_t total = 0, i = first, count = 0;
+  for (; i < l.count && count < kAdamTensors; ++i)
+    if (l.ns[i]) total += l.ns[i], ++count;
+  *next = i;
+  r.len = piece_values(total, count);
+  for (i = first; i < *next; ++i) {
+    if (l.ns[i] == 0) continue;
+    AdamTensor& e = r.tensors[r.count++];
+    e.p = l.params[i];
+    e.g = l.grads[i];
+    e.m = l.exp_avgs[i];
+    e.v = l.exp_avg_sqs[i];
+    e.scales = l.small() ? l.scales[i] : nullptr;
+    e.delta = l.deltas ? l.deltas[i] : nullptr;
+    e.n = (uint32_t)l.ns[i];
+    e.piece0_types = r.n | (uint32_t)l.types[i] << 28 | (uint32_t)l.grad_types[i] << 30;
+    r.n += (uint32_t)ceil_div(l.ns[i], r.len);
+  }
+  return r;
+}
+
+}  // namespace
+
+TLC_API int tlc_adamw(tlc_train* c, size_t count, void* const* params, const int* types,
+                      const size_t* ns, const void* const* grads, const int* grad_types,
+                      int state_type, void* const* exp_avgs, void* const* exp_avg_sqs,
+                      float* const* scales, float* const* deltas,
+                      const tlc_adamw_options* options, tlc_adamw_clock* clock,
+                      tlc_norm_result* result) {
+  const char* fn = "tlc_adamw";
+  int st = check_usable(c, fn);
+  if (st) return st;
+  const AdamCall l{count,       params, types,  ns,    grads, grad_types, state_type, exp_avgs,
+                   exp_avg_sqs, scales, deltas, clock, result};
+  st = check_options(fn, options, result != nullptr);
+  if (!st) st = check_adamw(c, fn, l);
+  if (st) return st;
+  DeviceScope dev(c->device);
+  st = dev.status();
+  if (st) return st;
+  AdamArgs a = {};
+  a.lr = options->lr;
+  a.log_beta1 = log(options->beta1);
+  a.log_beta2 = log(options->beta2);
+  a.decay = options->weight_decay;
+  a.c1 = (float)(1.0 - options->beta1);
+  a.c2 = (float)(1.0 - options->beta2);
+  a.eps = (float)options->eps;
+  a.max_norm = options->max_norm;
+  a.clock = clock;
+  a.result = result;
+  size_t next = 0;
+  do {
+    const AdamList list = adam_list(l, next, &next);
+    a.ticket = next >= count ? c->ticket : nullptr;
+    st = launched(c, launch_adamw(list, a, state_type, c->stream), fn);
+  } while (!st && next < count);
+  return st;
 }

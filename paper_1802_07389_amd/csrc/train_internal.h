@@ -1,7 +1,9 @@
-// train_internal.h -- definitions shared by the kernels of the embedding
-// tables and of the gradient norm and their host side (not part of the public
-// ABI).
+// train_internal.h -- definitions shared by the kernels of the training step
+// (embedding tables, gradient norm, token log probabilities, AdamW) and their host
+// side (not part of the public ABI).
 #pragma once
+
+#include <float.h>
 
 #include "tlc_internal.h"
 #include "typed_io.hpp"
@@ -186,5 +188,101 @@ hipError_t launch_norm_finish(const double* partials, uint32_t np, tlc_norm_resu
 template <class List>
 hipError_t launch_clip(const List& list, const double* partials, uint32_t np, float max_norm,
                        tlc_norm_result* result, hipStream_t st);
+
+// What a norm makes of the values.
+struct Clip {
+  float norm, coef;
+  bool finite;
+};
+__device__ __forceinline__ Clip clip_of(double sumsq, float max_norm) {
+  const double norm = sqrt(sumsq);
+  Clip c;
+  c.finite = sumsq >= 0.0 && sumsq <= DBL_MAX;  // false for NaN too
+  c.norm = (float)norm;
+  c.coef = !c.finite ? __builtin_nanf("")
+                     : (norm > (double)max_norm ? (float)((double)max_norm / norm) : 1.0f);
+  return c;
+}
+
+__device__ __forceinline__ void put_result(tlc_norm_result* r, Clip c) {
+  r->norm = c.norm;
+  r->coef = c.coef;
+  r->status = c.finite ? TLC_OK : TLC_E_NONFINITE;
+  r->reserved = 0u;
+}
+
+// ---- token log probabilities
+constexpr uint32_t kLogThreads = 256;
+// A row, or a part of one: its largest logit (at least -FLT_MAX) and sums by it.
+struct LogitPart {
+  float m, s0, s1;
+};
+struct LogitArgs {
+  const void* x;
+  uint64_t stride;  // values
+  uint32_t count, vocab;
+  float scale;
+  const void* targets;  // NULL: none
+  bool wide_ids;        // targets are int64
+  int64_t ignore;
+  uint32_t* bad;        // pinned host word: set where a target is outside the vocabulary
+};
+struct TokenArgs : LogitArgs {
+  tlc_token_result* results;
+  uint32_t top;
+  float* top_logprobs;
+  int32_t* top_ids;
+  // rows cut into parts: the parts' sums and `top` keys each
+  uint32_t parts, part_packs;
+  LogitPart* part;
+  uint64_t* keys;
+};
+// Parts of a row: where the rows alone leave CUs idle, as many as make
+// kLogBlocks blocks, each with a pack for every thread at least.
+constexpr uint32_t kLogBlocks = 1024, kLogMaxParts = kLogThreads;
+inline uint32_t logit_parts(uint32_t count, uint32_t packs) {
+  const uint32_t want = std::min(kLogBlocks / count, kLogMaxParts);
+  return std::max(1u, std::min(want, packs / kLogThreads));
+}
+hipError_t launch_token_logprobs(const TokenArgs& a, int type, hipStream_t st);
+
+struct TokenGradArgs : LogitArgs {
+  const tlc_token_result* results;
+  const float* grad_logprob;  // NULL: zeroes
+  const float* grad_entropy;  // NULL: zeroes
+  void* out;
+  uint64_t out_stride;
+  uint32_t slices;            // blocks of a row
+};
+hipError_t launch_token_grad(const TokenGradArgs& a, int type, int out_type, hipStream_t st);
+
+// ---- AdamW
+constexpr uint32_t kAdamThreads = 256;
+constexpr uint32_t kAdamTensors = 64;  // of a launch
+struct AdamTensor {
+  void* p;
+  const void* g;
+  void* m;
+  void* v;
+  float* scales;  // states in 8 bits: two floats a block
+  float* delta;   // or NULL
+  uint32_t n;
+  uint32_t piece0_types;  // its first piece, p's type in bits 28 and 29, g's in 30 and 31
+};
+struct AdamList {
+  uint32_t count, n;  // tensors, pieces
+  uint32_t len;       // values of a piece
+  AdamTensor tensors[kAdamTensors];
+};
+struct AdamArgs {
+  double lr, log_beta1, log_beta2, decay;
+  float c1, c2;  // 1 - beta
+  float eps, max_norm;
+  tlc_adamw_clock* clock;
+  tlc_norm_result* result;  // NULL: no clipping
+  uint32_t* ticket;         // the step's last launch: counts its blocks; else NULL
+};
+static_assert(sizeof(AdamList) + sizeof(AdamArgs) <= 3840, "kernel arguments end at 4096 bytes");
+hipError_t launch_adamw(const AdamList& list, const AdamArgs& a, int state_type, hipStream_t st);
 
 }  // namespace tlc

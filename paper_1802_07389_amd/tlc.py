@@ -67,6 +67,11 @@ TLC_MAX_ROWS = 2147483646
 TLC_MAX_DIM = 16777216
 TLC_CAPTURE_TENSORS = 128
 
+TLC_MAX_TOP = 64
+TLC_STATE_BLOCK = 256
+TLC_STATE_F32 = 0
+TLC_STATE_8BIT = 1
+
 EXPORTS = (
     "tlc_max_compressed_bytes", "tlc_ctx_create", "tlc_ctx_create_batch",
     "tlc_ctx_destroy", "tlc_compress", "tlc_compress_ex", "tlc_compress_batch",
@@ -77,6 +82,7 @@ EXPORTS = (
     "tlc_compress_noalloc", "tlc_ctx_set_epochs",
     "tlc_train_create", "tlc_train_destroy", "tlc_train_sync", "tlc_embedding",
     "tlc_embedding_grad", "tlc_grad_norm", "tlc_clip", "tlc_clip_grad_norm",
+    "tlc_token_logprobs", "tlc_token_logprobs_grad", "tlc_adamw",
 )
 
 
@@ -92,6 +98,27 @@ class tlc_norm_result(ctypes.Structure):
     host copy of it)."""
     _fields_ = [("sumsq", ctypes.c_double), ("norm", ctypes.c_float), ("coef", ctypes.c_float),
                 ("status", ctypes.c_int32), ("reserved", ctypes.c_uint32)]
+
+
+class tlc_token_result(ctypes.Structure):
+    """struct tlc_token_result of tlc.h (device memory; this layout reads a
+    host copy of it)."""
+    _fields_ = [("logprob", ctypes.c_float), ("entropy", ctypes.c_float),
+                ("max", ctypes.c_float), ("log_sum", ctypes.c_float)]
+
+
+class tlc_adamw_clock(ctypes.Structure):
+    """struct tlc_adamw_clock of tlc.h (device memory; this layout reads a
+    host copy of it)."""
+    _fields_ = [("step", ctypes.c_int64), ("lr_scale", ctypes.c_float),
+                ("reserved", ctypes.c_uint32)]
+
+
+class tlc_adamw_options(ctypes.Structure):
+    """struct tlc_adamw_options of tlc.h."""
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double),
+                ("max_norm", ctypes.c_float)]
 
 
 class TLCError(RuntimeError):
@@ -171,6 +198,15 @@ def _load():
     L.tlc_clip.restype = i
     L.tlc_clip_grad_norm.argtypes = [vp, sz, P(vp), P(i), P(sz), f, vp, P(vp)]
     L.tlc_clip_grad_norm.restype = i
+    L.tlc_token_logprobs.argtypes = [vp, vp, i, sz, sz, sz, f, vp, i, ctypes.c_int64, vp, sz, vp,
+                                     vp]
+    L.tlc_token_logprobs.restype = i
+    L.tlc_token_logprobs_grad.argtypes = [vp, vp, i, sz, sz, sz, f, vp, i, ctypes.c_int64, vp, vp,
+                                          vp, vp, i, sz]
+    L.tlc_token_logprobs_grad.restype = i
+    L.tlc_adamw.argtypes = [vp, sz, P(vp), P(i), P(sz), P(vp), P(i), i, P(vp), P(vp), P(vp),
+                            P(vp), P(tlc_adamw_options), vp, vp]
+    L.tlc_adamw.restype = i
     return L
 
 
@@ -334,6 +370,31 @@ def tlc_clip_grad_norm(ctx, tensors, types, ns, max_norm, result, outs=None):
     """outs: a list of device pointers, or None: in place."""
     return lib.tlc_clip_grad_norm(ctx, len(tensors), *_list_args(tensors, types, ns), max_norm,
                                   result, None if outs is None else _arr(ctypes.c_void_p, outs))
+
+
+def tlc_token_logprobs(ctx, logits, type_, count, vocab, stride, scale, targets, ids_type,
+                       ignore_id, results, top=0, top_logprobs=None, top_ids=None):
+    return lib.tlc_token_logprobs(ctx, logits, type_, count, vocab, stride, scale, targets,
+                                  ids_type, ignore_id, results, top, top_logprobs, top_ids)
+
+
+def tlc_token_logprobs_grad(ctx, logits, type_, count, vocab, stride, scale, targets, ids_type,
+                            ignore_id, results, grad_logprob, grad_entropy, out, out_type,
+                            out_stride):
+    return lib.tlc_token_logprobs_grad(ctx, logits, type_, count, vocab, stride, scale, targets,
+                                       ids_type, ignore_id, results, grad_logprob, grad_entropy,
+                                       out, out_type, out_stride)
+
+
+def tlc_adamw(ctx, params, types, ns, grads, grad_types, state_type, exp_avgs, exp_avg_sqs,
+              scales, deltas, options, clock, result=None):
+    """Lists of device pointers, types and value counts (scales, deltas: or
+    None); options: a tlc_adamw_options; clock, result: device addresses."""
+    ptrs = lambda v: None if v is None else _arr(ctypes.c_void_p, v)  # noqa: E731
+    return lib.tlc_adamw(ctx, len(params), *_list_args(params, types, ns), ptrs(grads),
+                         _arr(ctypes.c_int, grad_types), state_type, ptrs(exp_avgs),
+                         ptrs(exp_avg_sqs), ptrs(scales), ptrs(deltas),
+                         None if options is None else ctypes.byref(options), clock, result)
 
 
 def tlc_profile_enable(ctx, on):
@@ -583,9 +644,135 @@ class NormResult:
         self.status = self.buffer.view(torch.int32)[4]
 
 
+class TokenResult:
+    """tlc_token_results of the rows of one call in device memory, with views
+    of their fields, and the rows' alternatives (None where there are none)."""
+
+    def __init__(self, shape, top, device):
+        shape = tuple(shape)
+        self.buffer = torch.empty(*shape, 4, dtype=torch.float32, device=device)
+        self.logprob, self.entropy, self.max, self.log_sum = self.buffer.unbind(-1)
+        self.shape, self.top = shape, top
+        self.top_logprobs = self.top_ids = None
+        if top:
+            self.top_logprobs = torch.empty(*shape, top, dtype=torch.float32, device=device)
+            self.top_ids = torch.empty(*shape, top, dtype=torch.int32, device=device)
+
+
+def _dev_of(t, name, dtype, shape):
+    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be a contiguous {dtype} GPU tensor of shape {shape}")
+    return t.data_ptr()
+
+
+def _logit_rows(logits, targets):
+    """(arguments of the logits, of the targets, shape of the rows)."""
+    if logits.dim() < 2 or logits.shape[-1] == 0:
+        raise ValueError("logits must be rows of a vocabulary")
+    ptr, code, stride = _matrix(logits, "logits")
+    vocab, shape = logits.shape[-1], tuple(logits.shape[:-1])
+    ids, ids_code = None, TLC_I64
+    if targets is not None:
+        if tuple(targets.shape) != shape:
+            raise ValueError("targets must have the shape of the logits' rows")
+        ids, ids_code = _token_ids(targets)
+    count = 1
+    for n in shape:
+        count *= n
+    return (ptr, code, count, vocab, stride), (ids, ids_code), shape
+
+
+class AdamWList:
+    """Weights of one AdamW step with their states, laid out once.  A program
+    makes it once and keeps it: it keeps the tensors alive, and follows their
+    values, not a tensor that takes one's place.
+
+    exp_avgs, exp_avg_sqs
+                the states: float32, or (bits = 8) float8_e4m3fn and
+                float8_e5m2 tensors, a value being its number times its
+                block's scale
+    scales      8 bits: a float32 tensor [blocks, 2] for every weight; else None
+    step, lr_scale
+                views of the clock: steps done, and the factor of lr
+    """
+
+    def __init__(self, params, grads=None, bits=32, deltas=None, states=None, clock=None):
+        if bits not in (32, 8):
+            raise ValueError("states have 32 or 8 bits")
+        self.params, self.bits = list(params), bits
+        for p in self.params:
+            if not p.is_contiguous():
+                raise ValueError("every tensor of a list must be contiguous")
+        self.count = len(self.params)
+        self.ns = [p.numel() for p in self.params]
+        codes = [_type_of(p, "param") for p in self.params]
+        kinds = [torch.float32] * 2 if bits == 32 else [torch.float8_e4m3fn, torch.float8_e5m2]
+        blocks = [-(-n // TLC_STATE_BLOCK) for n in self.ns]
+        if states is None:
+            states = [[torch.zeros(p.shape, dtype=k, device=p.device) for p in self.params]
+                      for k in kinds]
+            states += [[torch.zeros(b, 2, device=p.device)
+                        for b, p in zip(blocks, self.params)]] if bits == 8 else []
+        if len(states) != (2 if bits == 32 else 3):
+            raise ValueError("states are exp_avgs, exp_avg_sqs and, in 8 bits, scales")
+        self.exp_avgs, self.exp_avg_sqs = list(states[0]), list(states[1])
+        self.scales = list(states[2]) if bits == 8 else None
+        self.clock = clock
+        if clock is None:
+            device = self.params[0].device if self.params else "cuda"
+            self.clock = torch.tensor([0, 0x3f800000], device=device)  # 0 steps, 1.0f
+        self.clock_ptr = _dev_of(self.clock, "clock", torch.int64, (2,))
+        self.step, self.lr_scale = self.clock[0], self.clock.view(torch.float32)[2]
+        self.deltas = None if deltas is None else list(deltas)
+        # the arguments of tlc_adamw around the gradients'
+        self.args = _list_args([p.data_ptr() for p in self.params], codes, self.ns)
+        ptrs = [self._ptrs(t, k, "state") for t, k in
+                zip([self.exp_avgs, self.exp_avg_sqs], kinds)]
+        scales = None
+        if bits == 8:
+            if len(self.scales) != self.count:
+                raise ValueError("params and scales differ in their number")
+            scales = _arr(ctypes.c_void_p, [_dev_of(s, "scales", torch.float32, (b, 2))
+                                            for s, b in zip(self.scales, blocks)])
+        self.state_args = (TLC_STATE_F32 if bits == 32 else TLC_STATE_8BIT, *ptrs, scales,
+                           None if deltas is None else self._ptrs(self.deltas, torch.float32,
+                                                                  "delta"))
+        self.grads = None if grads is None else list(grads)
+        self.grad_args = None if grads is None else self.lay_out(self.grads)
+        self.options, self.options_ptr, self.rates = None, None, None
+
+    def _ptrs(self, tensors, dtype, name):
+        if len(tensors) != self.count:
+            raise ValueError(f"params and {name}s differ in their number")
+        for t, n in zip(tensors, self.ns):
+            if t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or t.numel() != n:
+                raise ValueError(f"every {name} must be a contiguous {dtype} GPU tensor of its "
+                                 "weight's size")
+        return _arr(ctypes.c_void_p, [t.data_ptr() for t in tensors])
+
+    def lay_out(self, grads):
+        """The arguments of the gradients, one for every weight."""
+        grads = list(grads)
+        if [g.numel() for g in grads] != self.ns:
+            raise ValueError("params and grads differ in their sizes")
+        for g in grads:
+            if not g.is_contiguous():
+                raise ValueError("every tensor of a list must be contiguous")
+        return (_arr(ctypes.c_void_p, [g.data_ptr() for g in grads]),
+                _arr(ctypes.c_int, [_type_of(g, "grad") for g in grads]))
+
+    def lay_out_options(self, *rates):
+        """The options' argument, made again where they change."""
+        if rates != self.rates:
+            self.options, self.rates = tlc_adamw_options(*rates), rates
+            self.options_ptr = ctypes.byref(self.options)
+        return self.options_ptr
+
+
 class TrainContext:
     """The training-step operators around the codec, on one stream: embedding
-    lookups and gradients, the gradient norm and clipping.  Work is ordered on
+    lookups and gradients, the gradient norm and clipping, token log
+    probabilities and their gradient, AdamW.  Work is ordered on
     that stream (by default torch's current one when the context is made):
     tensors that another stream makes or uses, and replays of captured calls on
     another stream, are waited for by the caller.  The calls are not part of
@@ -685,6 +872,75 @@ class TrainContext:
                                       out_ptrs))
         return r
 
+    def token_result(self, shape, top=0):
+        """A result buffer for rows of `shape` (a number or a shape) with `top`
+        alternatives each, to pass to token_logprobs()."""
+        with torch.cuda.stream(self.stream):
+            return TokenResult([shape] if isinstance(shape, int) else shape, top, self.device)
+
+    def token_logprobs(self, logits, targets=None, scale=1.0, ignore_id=-100, top=0, out=None):
+        """Log probabilities of targets (one for every row of logits), the
+        rows' entropies and their `top` most likely alternatives."""
+        rows, ids, shape = _logit_rows(logits, targets)
+        if out is None:
+            out = self.token_result(shape, top)
+        elif out.shape != shape or out.top != top:
+            raise ValueError("out has the wrong size")
+        _check(lib.tlc_token_logprobs(
+            self.handle, *rows, scale, *ids, ignore_id, out.buffer.data_ptr(), top,
+            out.top_logprobs.data_ptr() if top else None, out.top_ids.data_ptr() if top else None))
+        return out
+
+    def token_logprobs_grad(self, logits, targets, results, grad_logprob=None, grad_entropy=None,
+                            scale=1.0, ignore_id=-100, out=None, dtype=None):
+        """The gradient of logits from those of token_logprobs()' log
+        probabilities and entropies.  results: its TokenResult, or the float32
+        buffer of one; out: may be logits itself (by default a new tensor of
+        `dtype`, or the logits' type)."""
+        rows, ids, shape = _logit_rows(logits, targets)
+        buffer = results.buffer if isinstance(results, TokenResult) else results
+        if out is None:
+            with torch.cuda.stream(self.stream):
+                out = torch.empty(logits.shape, dtype=dtype or logits.dtype, device=self.device)
+        elif out.shape != logits.shape:
+            raise ValueError("out has the wrong size")
+        grads = [None if g is None else _dev_of(g, name, torch.float32, shape) for g, name in
+                 ((grad_logprob, "grad_logprob"), (grad_entropy, "grad_entropy"))]
+        out_ptr, out_code, out_stride = _matrix(out, "out")
+        _check(lib.tlc_token_logprobs_grad(
+            self.handle, *rows, scale, *ids, ignore_id,
+            _dev_of(buffer, "results", torch.float32, (*shape, 4)), *grads, out_ptr, out_code,
+            out_stride))
+        return out
+
+    def adamw_list(self, params, grads=None, bits=32, deltas=None, states=None, clock=None):
+        """The weights of an AdamW step with their states, laid out once.
+        grads: where they keep their buffers; deltas: float32 tensors for the
+        weights' change (a gradient itself, where it is float32); states:
+        (exp_avgs, exp_avg_sqs[, scales]) and clock, by default new ones of
+        zeroes."""
+        with torch.cuda.stream(self.stream):
+            return AdamWList(params, grads, bits, deltas, states, clock)
+
+    def adamw(self, weights, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, grads=None,
+              max_norm=None, result=None):
+        """One step of AdamW (asynchronous) over an AdamWList, with the grads
+        given here or kept in it.  max_norm: the gradients are taken clipped by
+        result.sumsq, which grad_norm() (and a sum over ranks) left there; where
+        that is not finite the step is left out."""
+        if (max_norm is None) != (result is None):
+            raise ValueError("max_norm and result belong together")
+        grad_args = weights.grad_args if grads is None else weights.lay_out(grads)
+        if grad_args is None:
+            raise ValueError("no gradients are given, and the list has none")
+        options = weights.lay_out_options(lr, beta1, beta2, eps, weight_decay,
+                                          0.0 if max_norm is None else max_norm)
+        _check(lib.tlc_adamw(self.handle, weights.count, *weights.args, *grad_args,
+                             *weights.state_args, options, weights.clock_ptr,
+                             None if result is None else result.ptr))
+        return weights
+
     def sync(self):
-        """Wait; raises TLCError(TLC_E_INDEX) after an id outside its table."""
+        """Wait; raises TLCError(TLC_E_INDEX) after an id outside its table or
+        vocabulary."""
         _check(tlc_train_sync(self.handle))
