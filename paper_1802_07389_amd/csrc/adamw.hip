@@ -8,6 +8,8 @@
 // fp32 states, 16 of 8 bits).
 #include <math.h>
 
+#include <type_traits>
+
 #include "device_common.hpp"
 #include "train_internal.h"
 #include "typed_io.hpp"
@@ -48,60 +50,69 @@ __device__ __forceinline__ float adam_step(float p, float g, float& m, float& v,
 }
 
 constexpr int V = 4;  // neighbouring values of a thread
+constexpr uint32_t kStride = kAdamThreads * V;
+// Of them, in flight: a wave's are whole blocks of 8-bit states (100M values, two |
+// four: 590 | 569 us of 32 bits, 330 | 332 of 8, one 363; few values, which have no
+// wave to spare, in short pieces one at a time).
+constexpr uint32_t steps_of(int bits) { return bits == 32 ? 4 : 2; }
 
-// Values k to k + 3 of x, those from n on 0.
-template <class T>
-__device__ __forceinline__ Pack<T, V> load_some(const T* x, uint32_t k, uint32_t n) {
-  if (n - k >= V) return load_pack<T, V>(x + k);
-  Pack<T, V> r = {};
+// Values k to k + 3 of x, those from n on 0.  No load waits for a condition: at
+// the end a pack is moved back to end with the values, and its own ones shifted
+// down; of fewer values than a pack, value by value.
+template <bool kFull, class T>
+__device__ __forceinline__ Pack<T, V> load_some(const void* x, uint32_t k, uint32_t n) {
+  const T* p = static_cast<const T*>(x);
+  if (kFull) return load_pack<T, V>(p + k);
+  Pack<T, V> r;
+  if (n < V) {
 #pragma unroll
-  for (uint32_t e = 0; e < V; ++e)
-    if (e < n - k) r.v[e] = x[k + e];
+    for (uint32_t e = 0; e < V; ++e) {
+      r.v[e] = p[umin32(k + e, n - 1)];
+      if (k + e >= n) r.v[e] = T();
+    }
+    return r;
+  }
+  const uint32_t at = umin32(k, n - V), skip = k - at;
+  const Pack<T, V> c = load_pack<T, V>(p + at);
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (uint32_t e = 0; e < V; ++e) {
+      r.v[e] = T();
+#pragma unroll
+      for (uint32_t s = V - e; s-- > 0;) r.v[e] = skip == s ? c.v[e + s] : r.v[e];
+    }
+  } else {
+    using Word = std::conditional_t<sizeof(T) == 2, uint64_t, uint32_t>;
+    const Word w = skip < V ? __builtin_bit_cast(Word, c.v) >> (8 * sizeof(T) * skip) : 0;
+    r.v = __builtin_bit_cast(decltype(r.v), w);
+  }
   return r;
 }
-template <class T>
-__device__ __forceinline__ void store_some(T* x, uint32_t k, uint32_t n, const Pack<T, V>& r) {
-  if (n - k >= V) {
-    store_pack<T, V>(x + k, r);
+template <bool kFull, class T>
+__device__ __forceinline__ void store_some(void* x, uint32_t k, uint32_t n, const Pack<T, V>& r) {
+  T* p = static_cast<T*>(x);
+  if (kFull || k + V <= n) {
+    store_pack<T, V>(p + k, r);
     return;
   }
 #pragma unroll
   for (uint32_t e = 0; e < V; ++e)
-    if (e < n - k) x[k + e] = r.v[e];
-}
-
-// Four codes as one word, those from n on 0.
-__device__ __forceinline__ uint32_t load_codes(const uint8_t* x, uint32_t k, uint32_t n) {
-  if (n - k >= V) return ld_word(x + k);
-  uint32_t w = 0;
-#pragma unroll
-  for (uint32_t e = 0; e < V; ++e)
-    if (e < n - k) w |= (uint32_t)x[k + e] << (8 * e);
-  return w;
-}
-__device__ __forceinline__ void store_codes(uint8_t* x, uint32_t k, uint32_t n, uint32_t w) {
-  if (n - k >= V) {
-    st_word(x + k, w);
-    return;
-  }
-#pragma unroll
-  for (uint32_t e = 0; e < V; ++e)
-    if (e < n - k) x[k + e] = (uint8_t)(w >> (8 * e));
+    if (k + e < n) p[k + e] = r.v[e];
 }
 
 // The code of y >= 0 in a format of kMantissa bits with smallest exponent kLowest
 // (below it steps are even) and largest code kMost: the codes joined by straight
 // lines make y a place between two of them, which `dither` (of the 23 - kMantissa
-// bits that are cut off) carries to the upper one as often as y is near it.
+// bits that are cut off) carries to the upper one as often as y is near it.  At
+// least `least`.
 template <int kMantissa, int kLowest, uint32_t kMost>
-__device__ __forceinline__ uint32_t fp8_code(float y, uint32_t dither) {
+__device__ __forceinline__ uint32_t fp8_code(float y, uint32_t dither, uint32_t least) {
   constexpr int kCut = 23 - kMantissa;
   constexpr float kUnit = 1.0f / (float)(1ull << -kLowest);  // 2^kLowest
-  const uint32_t fine =
-      ((__float_as_uint(y) + dither) >> kCut) - ((uint32_t)(126 + kLowest) << kMantissa);
   constexpr float kFine = (float)(1ull << (kMantissa - kLowest + kCut));
-  const uint32_t small = ((uint32_t)(fminf(y, kUnit) * kFine) + dither) >> kCut;
-  return umin32(y < kUnit ? small : fine, kMost);
+  const uint32_t fine = __float_as_uint(y) - ((uint32_t)(126 + kLowest) << 23);
+  const uint32_t small = (uint32_t)(fminf(y, kUnit) * kFine);
+  return umin32(umax32(((y < kUnit ? small : fine) + dither) >> kCut, least), kMost);
 }
 
 // A block's scale from its largest magnitude (as bits): its share of the
@@ -113,192 +124,268 @@ __device__ __forceinline__ float scale_of_max(uint32_t bits, float inv_most) {
   return fmaxf(__uint_as_float(bits) * inv_most, 0x1p-126f);
 }
 
-constexpr uint32_t kDitherK = 0xC13FA9A9u, kDitherT = 0x91E10DA5u;
-
-// A piece of a tensor: its values from k0 on.
-struct AdamPiece {
-  void* p;
-  const void* g;
-  void* m;
-  void* v;
-  float* scales;
-  float* delta;
-  uint32_t k0, n;
+// x / s of many x >= 0 by one s, rounded as a division: the residual of a quotient
+// that is within a unit in the last place, times the rounded reciprocal, corrects
+// it (Markstein, IBM J. Res. Dev. 34, 1990), and one such step before brings the product with
+// the reciprocal there.  Residuals are exact where they do not underflow: of x below
+// 2^-102, whose quotient no code tells from 0 for s from 2^-64 on; for other s, a
+// division.
+struct Divisor {
+  float s, r;
+  bool exact;
+  __device__ __forceinline__ explicit Divisor(float scale)
+      : s(scale), r(1.0f / scale), exact(scale >= 0x1p-64f && scale <= 0x1p100f) {}
+  __device__ __forceinline__ float of(float x) const {
+    float q = x * r;
+    q = __builtin_fmaf(__builtin_fmaf(-q, s, x), r, q);
+    return __builtin_fmaf(__builtin_fmaf(-q, s, x), r, q);
+  }
 };
 
-// Values k to k + 3 of a piece.
-template <class P, class G, int kBits>
-__device__ __forceinline__ void step_four(const AdamPiece& t, uint32_t k, const AdamArgs& a,
-                                          const Factors& f) {
-  const bool in = k < t.n;  // of 8 bits the whole wave stays for its block's largest
-  if (kBits == 32 && !in) return;
-  float m[V] = {}, v[V] = {};
-  Pack<P, V> p = {};
-  Pack<G, V> g = {};
-  if (in) {
-    p = load_some(static_cast<const P*>(t.p), k, t.n);
-    g = load_some(static_cast<const G*>(t.g), k, t.n);
+constexpr uint32_t kDitherK = 0xC13FA9A9u, kDitherT = 0x91E10DA5u;
+
+// What a thread reads of a chunk.
+template <class P, class G, int kBits, uint32_t kSteps>
+struct Chunk {
+  Pack<P, V> p[kSteps];
+  Pack<G, V> g[kSteps];
+  Pack<std::conditional_t<kBits == 32, float, uint8_t>, V> m[kSteps], v[kSteps];
+  float sm[kSteps], sv[kSteps];
+};
+
+template <bool kFull, class P, class G, int kBits, uint32_t kSteps>
+__device__ __forceinline__ void load_chunk(Chunk<P, G, kBits, kSteps>& c, const AdamPiece& t,
+                                           uint32_t k0) {
+  using S = std::conditional_t<kBits == 32, float, uint8_t>;
+#pragma unroll
+  for (uint32_t u = 0; u < kSteps; ++u) {
+    const uint32_t k = k0 + u * kStride + threadIdx.x * V;
+    c.p[u] = load_some<kFull, P>(t.p, k, t.n);
+    c.g[u] = load_some<kFull, G>(t.g, k, t.n);
+    c.m[u] = load_some<kFull, S>(t.m, k, t.n);
+    c.v[u] = load_some<kFull, S>(t.v, k, t.n);
+    if constexpr (kBits == 8) {
+      // (a wave beyond the end takes the last block's: its values are 0)
+      const uint32_t b = umin32(k, t.n - 1) / TLC_STATE_BLOCK;
+      c.sm[u] = t.scales[b * 2];
+      c.sv[u] = t.scales[b * 2 + 1];
+    }
+  }
+}
+
+template <bool kFull, class P, class G, int kBits, uint32_t kSteps>
+__device__ __forceinline__ void step_chunk(const Chunk<P, G, kBits, kSteps>& c,
+                                           const AdamPiece& t, uint32_t k0, const AdamArgs& a,
+                                           const Factors& f) {
+  using S = std::conditional_t<kBits == 32, float, uint8_t>;
+#pragma unroll
+  for (uint32_t u = 0; u < kSteps; ++u) {
+    const uint32_t k = k0 + u * kStride + threadIdx.x * V;
+    float m[V], v[V];
     if constexpr (kBits == 32) {
-      const Pack<float, V> pm = load_some(static_cast<const float*>(t.m), k, t.n);
-      const Pack<float, V> pv = load_some(static_cast<const float*>(t.v), k, t.n);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        m[e] = pm.get(e);
-        v[e] = pv.get(e);
+        m[e] = c.m[u].get(e);
+        v[e] = c.v[u].get(e);
       }
     } else {
-      const int wm = (int)load_codes(static_cast<const uint8_t*>(t.m), k, t.n);
-      const int wv = (int)load_codes(static_cast<const uint8_t*>(t.v), k, t.n);
-      const float* s = t.scales + k / TLC_STATE_BLOCK * 2;
-      const float sm = s[0], sv = s[1];
-      m[0] = __builtin_amdgcn_cvt_f32_fp8(wm, 0) * sm;
-      m[1] = __builtin_amdgcn_cvt_f32_fp8(wm, 1) * sm;
-      m[2] = __builtin_amdgcn_cvt_f32_fp8(wm, 2) * sm;
-      m[3] = __builtin_amdgcn_cvt_f32_fp8(wm, 3) * sm;
-      v[0] = __builtin_amdgcn_cvt_f32_bf8(wv, 0) * sv;
-      v[1] = __builtin_amdgcn_cvt_f32_bf8(wv, 1) * sv;
-      v[2] = __builtin_amdgcn_cvt_f32_bf8(wv, 2) * sv;
-      v[3] = __builtin_amdgcn_cvt_f32_bf8(wv, 3) * sv;
-    }
-  }
-  Pack<P, V> q;
-  Pack<float, V> d;
+      const int wm = __builtin_bit_cast(int, c.m[u].v), wv = __builtin_bit_cast(int, c.v[u].v);
+      const auto m01 = __builtin_amdgcn_cvt_pk_f32_fp8(wm, false);
+      const auto m23 = __builtin_amdgcn_cvt_pk_f32_fp8(wm, true);
+      const auto v01 = __builtin_amdgcn_cvt_pk_f32_bf8(wv, false);
+      const auto v23 = __builtin_amdgcn_cvt_pk_f32_bf8(wv, true);
+      const float cm[V] = {m01[0], m01[1], m23[0], m23[1]};
+      const float cv[V] = {v01[0], v01[1], v23[0], v23[1]};
 #pragma unroll
-  for (int e = 0; e < V; ++e) {
-    const float old = p.get(e);
-    q.set(e, adam_step(old, f.coef * g.get(e), m[e], v[e], a, f));
-    d.set(e, q.get(e) - old);
-  }
-  if (in) {
-    store_some(static_cast<P*>(t.p), k, t.n, q);
-    if (t.delta) store_some(t.delta, k, t.n, d);
-  }
-  if constexpr (kBits == 32) {
-    Pack<float, V> pm, pv;
+      for (int e = 0; e < V; ++e) {
+        m[e] = cm[e] * c.sm[u];
+        v[e] = cv[e] * c.sv[u];
+      }
+    }
+    Pack<P, V> q;
+    Pack<float, V> d;
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      pm.set(e, m[e]);
-      pv.set(e, v[e]);
+      const float old = c.p[u].get(e);
+      q.set(e, adam_step(old, f.coef * c.g[u].get(e), m[e], v[e], a, f));
+      d.set(e, q.get(e) - old);
     }
-    store_some(static_cast<float*>(t.m), k, t.n, pm);
-    store_some(static_cast<float*>(t.v), k, t.n, pv);
-  } else {
-    uint32_t mm = 0, mv = 0;
+    store_some<kFull, P>(t.p, k, t.n, q);
+    if (t.delta) store_some<kFull, float>(t.delta, k, t.n, d);
+    Pack<S, V> pm, pv;
+    if constexpr (kBits == 32) {
 #pragma unroll
-    for (int e = 0; e < V; ++e)
-      if (k + e < t.n) {  // beyond the end nothing is held
+      for (int e = 0; e < V; ++e) {
+        pm.set(e, m[e]);
+        pv.set(e, v[e]);
+      }
+    } else {
+      uint32_t mm = 0, mv = 0;  // (values beyond the end are 0)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
         mm = umax32(mm, abs_bits(m[e]));
         mv = umax32(mv, abs_bits(v[e]));
       }
-    const float sm = scale_of_max(wave_max(mm), 1.0f / 448.0f);
-    const float sv = scale_of_max(wave_max(mv), 1.0f / 57344.0f);
-    uint32_t wm = 0, wv = 0;
+      const float sm = scale_of_max(wave_max(mm), 1.0f / 448.0f);  // the wave's, in scalars
+      const float sv = scale_of_max(wave_max(mv), 1.0f / 57344.0f);
+      float ym[V], yv[V];
+      const Divisor dm(sm), dv(sv);
+      if (dm.exact && dv.exact) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      const uint32_t h = (t.k0 + k + e) * kDitherK + f.step * kDitherT;
-      const float ym = sm > 0.0f ? fabsf(m[e]) / sm : 0.0f;
-      const float yv = sv > 0.0f ? v[e] / sv : 0.0f;
-      uint32_t qm = fp8_code<3, -6, 126>(ym, h >> 12);
-      uint32_t qv = fp8_code<2, -14, 123>(yv, (h ^ 0x80000000u) >> 11);
-      qm |= __float_as_uint(m[e]) >> 31 << 7;
-      if (qv == 0 && v[e] > 0.0f) qv = 1;  // a nonzero v stays one
-      if (!(sm >= 0.0f)) qm = 0;
-      if (!(sv >= 0.0f)) qv = 0;
-      wm |= qm << (8 * e);
-      wv |= qv << (8 * e);
-    }
-    if (in) {
-      store_codes(static_cast<uint8_t*>(t.m), k, t.n, wm);
-      store_codes(static_cast<uint8_t*>(t.v), k, t.n, wv);
-      if (k % TLC_STATE_BLOCK == 0) {
+        for (int e = 0; e < V; ++e) {
+          ym[e] = dm.of(fabsf(m[e]));
+          yv[e] = dv.of(v[e]);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          ym[e] = sm > 0.0f ? fabsf(m[e]) / sm : 0.0f;
+          yv[e] = sv > 0.0f ? v[e] / sv : 0.0f;
+        }
+      }
+      uint32_t wm = 0, wv = 0;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const uint32_t h = (t.k0 + k + e) * kDitherK + f.step * kDitherT;
+        // a nonzero v stays one
+        const uint32_t qm = fp8_code<3, -6, 126>(ym[e], h >> 12, 0u);
+        const uint32_t qv = fp8_code<2, -14, 123>(yv[e], (h ^ 0x80000000u) >> 11,
+                                                  umin32(__float_as_uint(v[e]), 1u));
+        wm |= (qm | (__float_as_uint(m[e]) >> 24 & 0x80u)) << (8 * e);
+        wv |= qv << (8 * e);
+      }
+      if (!(sm >= 0.0f)) wm = 0;
+      if (!(sv >= 0.0f)) wv = 0;
+      pm.v = __builtin_bit_cast(decltype(pm.v), wm);
+      pv.v = __builtin_bit_cast(decltype(pv.v), wv);
+      if (k % TLC_STATE_BLOCK == 0 && (kFull || k < t.n)) {
         t.scales[k / TLC_STATE_BLOCK * 2] = sm;
         t.scales[k / TLC_STATE_BLOCK * 2 + 1] = sv;
       }
     }
+    store_some<kFull, S>(t.m, k, t.n, pm);
+    store_some<kFull, S>(t.v, k, t.n, pv);
   }
 }
 
-template <class P, class G, int kBits>
-__device__ __forceinline__ void step_piece(const AdamTensor& t, uint32_t k0, uint32_t len,
-                                           const AdamArgs& a, const Factors& f) {
-  constexpr uint32_t kState = kBits == 32 ? 4 : 1;
-  AdamPiece r;
-  r.p = static_cast<P*>(t.p) + k0;
-  r.g = static_cast<const G*>(t.g) + k0;
-  r.m = static_cast<uint8_t*>(t.m) + (uint64_t)k0 * kState;
-  r.v = static_cast<uint8_t*>(t.v) + (uint64_t)k0 * kState;
-  r.scales = t.scales + k0 / TLC_STATE_BLOCK * 2;
-  r.delta = t.delta ? t.delta + k0 : nullptr;
-  r.k0 = k0;
-  r.n = umin32(len, t.n - k0);
-  for (uint32_t k = 0; k < r.n; k += kAdamThreads * V)
-    step_four<P, G, kBits>(r, k + threadIdx.x * V, a, f);
+// Piece i of a list, with pointers to its values.
+__device__ __forceinline__ AdamPiece piece_of(const AdamPinned& list, uint32_t i) {
+  return list.pieces[i];
 }
+__device__ __forceinline__ AdamPiece piece_of(const AdamList& list, uint32_t i) {
+  const uint32_t lane = threadIdx.x & 63u;
+  const uint32_t s = (uint32_t)__popcll(__ballot(
+      lane < list.count && (list.tensors[lane].piece0_types & 0xfffffffu) <= i));
+  const AdamTensor& t = list.tensors[uniform32(s) - 1];
+  return adam_piece(t, t.piece0_types >> 28, (i - (t.piece0_types & 0xfffffffu)) * list.len,
+                    list.len, list.state_bytes);
+}
+
+// Whether this block is the last one to have read the clock, whose value `step`
+// is here.  Blocks count themselves in groups, and the last of each group the
+// groups: one word for all took 8 ns a block (977 blocks of 1024 values 16.8 us).
+__device__ __forceinline__ bool last_to_read(uint32_t* tickets, int64_t step) {
+  uint32_t one = 1u;
+  asm volatile("" : "+v"(one) : "v"((uint32_t)step));  // the read is done before the count
+  const uint32_t groups = umin32(gridDim.x, kTicketGroups), g = blockIdx.x % groups;
+  uint32_t* mine = tickets + (1 + g) * kTicketWords;
+  if (atomicAdd(mine, one) != (gridDim.x - g + groups - 1) / groups - 1) return false;
+  *mine = 0u;
+  if (atomicAdd(tickets, 1u) != groups - 1) return false;
+  *tickets = 0u;
+  return true;
+}
+
+template <int kBits>
+struct Step {
+  const AdamArgs& a;
+  Factors* shared;
+  Factors f;
+  bool ready = false;
+
+  // The step's factors, which wave 0 has left in LDS.
+  __device__ __forceinline__ void wait() {
+    if (ready) return;
+    __syncthreads();
+    f = *shared;
+    ready = true;
+  }
+
+  template <class P, class G, uint32_t kSteps, bool kFull>
+  __device__ __forceinline__ void chunk(const AdamPiece& t, uint32_t k) {
+    Chunk<P, G, kBits, kSteps> c;
+    load_chunk<kFull>(c, t, k);
+    wait();
+    if (f.skip) {
+      // a change of nothing, so that the codec is not given the last step's
+      if (t.delta)
+#pragma unroll
+        for (uint32_t u = 0; u < kSteps; ++u)
+          store_some<kFull, float>(t.delta, k + u * kStride + threadIdx.x * V, t.n, {});
+      return;
+    }
+    step_chunk<kFull>(c, t, k, a, f);
+  }
+
+  template <class P, class G>
+  __device__ __forceinline__ void piece(const AdamPiece& t) {
+    constexpr uint32_t kSteps = steps_of(kBits);
+    uint32_t k = 0;
+    for (; t.n - k >= kSteps * kStride; k += kSteps * kStride) chunk<P, G, kSteps, true>(t, k);
+    for (; t.n - k >= kStride; k += kStride) chunk<P, G, 1, true>(t, k);
+    if (k < t.n) chunk<P, G, 1, false>(t, k);
+  }
+  template <class P>
+  __device__ __forceinline__ void piece(const AdamPiece& t) {
+    const uint32_t type = t.types >> 2;
+    if (type == TLC_F32)
+      piece<P, float>(t);
+    else if (type == TLC_BF16)
+      piece<P, bf16_t>(t);
+    else
+      piece<P, f16_t>(t);
+  }
+};
 
 }  // namespace
 
-template <int kBits>
-__global__ __launch_bounds__(kAdamThreads) void tlc_adamw_kernel(AdamList list, AdamArgs a) {
+template <class List, int kBits>
+__global__ __launch_bounds__(kAdamThreads) void tlc_adamw_kernel(List list, AdamArgs a) {
   __shared__ Factors shared;
+  const uint32_t i0 = (uint32_t)((uint64_t)blockIdx.x * list.n / gridDim.x);
+  const uint32_t i1 = (uint32_t)((uint64_t)(blockIdx.x + 1) * list.n / gridDim.x);
+  AdamPiece t = {};
+  if (i0 < i1) t = piece_of(list, i0);  // asked for first: it may be in host memory
   if (threadIdx.x == 0) {
     const int64_t step = a.clock->step + 1;
     shared = factors_of(a, step);
     if (a.result && blockIdx.x == 0) put_result(a.result, clip_of(a.result->sumsq, a.max_norm));
-    if (a.ticket) {
-      // the block that is last to have read the clock sets it; the read is done
-      // when its value is added
-      uint32_t one = 1u;
-      asm volatile("" : "+v"(one) : "v"((uint32_t)step), "v"(shared.coef));
-      if (atomicAdd(a.ticket, one) == gridDim.x - 1) {
-        if (!shared.skip) a.clock->step = step;
-        *a.ticket = 0u;
-      }
-    }
+    if (a.tickets && last_to_read(a.tickets, step) && !shared.skip) a.clock->step = step;
   }
-  __syncthreads();
-  const Factors f = shared;
-  const uint32_t lane = threadIdx.x & 63u;
-  for (uint32_t i = blockIdx.x; i < list.n; i += gridDim.x) {
-    const uint32_t s = (uint32_t)__popcll(__ballot(
-        lane < list.count && (list.tensors[lane].piece0_types & 0xfffffffu) <= i));
-    const AdamTensor& t = list.tensors[uniform32(s) - 1];
-    const uint32_t k0 = (i - (t.piece0_types & 0xfffffffu)) * list.len;
-    if (f.skip) {
-      // a change of nothing, so that the codec is not given the last step's
-      const uint32_t n = umin32(list.len, t.n - k0);
-      if (t.delta)
-        for (uint32_t k = threadIdx.x; k < n; k += kAdamThreads) t.delta[(uint64_t)k0 + k] = 0.0f;
-      continue;
-    }
-    const auto with = [&](auto p, auto g) {
-      step_piece<decltype(p), decltype(g), kBits>(t, k0, list.len, a, f);
-    };
-    const auto with_p = [&](auto p) {
-      const uint32_t type = t.piece0_types >> 30;
-      if (type == TLC_F32)
-        with(p, float());
-      else if (type == TLC_BF16)
-        with(p, bf16_t());
-      else
-        with(p, f16_t());
-    };
-    const uint32_t type = (t.piece0_types >> 28) & 3u;
+  Step<kBits> s{a, &shared, {}};
+  for (uint32_t i = i0; i < i1; ++i) {
+    if (i > i0) t = piece_of(list, i);
+    const uint32_t type = t.types & 3u;
     if (type == TLC_F32)
-      with_p(float());
+      s.template piece<float>(t);
     else if (type == TLC_BF16)
-      with_p(bf16_t());
+      s.template piece<bf16_t>(t);
     else
-      with_p(f16_t());
+      s.template piece<f16_t>(t);
   }
 }
 
-hipError_t launch_adamw(const AdamList& list, const AdamArgs& a, int state_type, hipStream_t st) {
+template <class List>
+hipError_t launch_adamw(const List& list, const AdamArgs& a, int state_type, hipStream_t st) {
   const uint32_t grid = std::max(1u, std::min(list.n, kNormBlocks));
   if (state_type == TLC_STATE_8BIT)
-    launch_k(tlc_adamw_kernel<8>, grid, kAdamThreads, st, list, a);
+    launch_k(tlc_adamw_kernel<List, 8>, grid, kAdamThreads, st, list, a);
   else
-    launch_k(tlc_adamw_kernel<32>, grid, kAdamThreads, st, list, a);
+    launch_k(tlc_adamw_kernel<List, 32>, grid, kAdamThreads, st, list, a);
   return hipGetLastError();
 }
+
+template hipError_t launch_adamw(const AdamList&, const AdamArgs&, int, hipStream_t);
+template hipError_t launch_adamw(const AdamPinned&, const AdamArgs&, int, hipStream_t);
 
 }  // namespace tlc

@@ -19,6 +19,8 @@ namespace {
 // last call guards the group (an event a call cost the host more than the
 // pieces).
 constexpr int kGroups = 2, kGroupSlots = 4;
+constexpr size_t kSlotPiece = sizeof(AdamPiece);  // bytes of the largest piece
+static_assert(sizeof(Piece) <= kSlotPiece, "slots hold pieces of either kind");
 constexpr size_t kMaxListValues = (size_t)1 << 40;
 constexpr float kMaxLogitScale = 1e18f;
 
@@ -49,18 +51,18 @@ struct tlc_train {
   // pinned: the sticky index flag and the staging slots of the pieces
   uint32_t* bad = nullptr;
   uint32_t* bad_dev = nullptr;
-  Piece* staging = nullptr;
-  Piece* staging_dev = nullptr;  // the same, as the device addresses it
+  uint8_t* staging = nullptr;
+  uint8_t* staging_dev = nullptr;  // the same, as the device addresses it
   size_t slot_pieces = 0;
   hipEvent_t group_done[kGroups] = {};
   bool group_used[kGroups] = {};
   int slot_next = 0;
   // host tables, reserved at creation so that the calls do not allocate
   std::vector<Span> spans, spans_ok, adamw_ok;
-  // token log probabilities: the parts of cut rows; AdamW: the last launch's ticket
+  // token log probabilities: the parts of cut rows; AdamW: the blocks' tickets
   LogitPart* logit_part = nullptr;
   uint64_t* logit_keys = nullptr;
-  uint32_t* ticket = nullptr;
+  uint32_t* tickets = nullptr;
 };
 
 namespace {
@@ -94,15 +96,17 @@ int check_table(const char* fn, size_t rows, size_t dim, int ids_type, int value
 }
 
 // The next pinned slot: a group's first one waits for the group's last calls.
-int take_slot(tlc_train* c, Piece** host, const Piece** dev) {
+template <class P>
+int take_slot(tlc_train* c, P** host, const P** dev) {
   const int slot = c->slot_next, group = slot / kGroupSlots;
   if (slot % kGroupSlots == 0 && c->group_used[group]) {
     const hipError_t e = hipEventSynchronize(c->group_done[group]);
     if (e != hipSuccess) return hip_fail(e, "hipEventSynchronize(staging)");
     c->group_used[group] = false;
   }
-  *host = c->staging + (size_t)slot * c->slot_pieces;
-  *dev = c->staging_dev + (size_t)slot * c->slot_pieces;
+  const size_t at = (size_t)slot * c->slot_pieces * kSlotPiece;
+  *host = reinterpret_cast<P*>(c->staging + at);
+  *dev = reinterpret_cast<const P*>(c->staging_dev + at);
   return TLC_OK;
 }
 
@@ -253,12 +257,13 @@ TLC_API int tlc_train_create(tlc_train** out, size_t max_tokens, size_t max_rows
     delete c;
     return hip_fail(e, "hipGetDevice");
   }
-  c->slot_pieces = max_tensors > kArgTensors ? kNormBlocks + max_tensors : 0;
-  // layout: partial sums | ticket | logits' parts | their keys | a long list's pieces |
+  c->slot_pieces =
+      max_tensors > std::min(kArgTensors, kAdamTensors) ? kNormBlocks + max_tensors : 0;
+  // layout: partial sums | tickets | logits' parts | their keys | a long list's pieces |
   //         sorted tokens, twice | counts of the sort | touched rows | partial rows
   size_t off = round_up(kNormBlocks * sizeof(double), 256);
-  const size_t off_ticket = off;
-  off += 256;
+  const size_t off_tickets = off;
+  off = round_up(off + kTicketBytes, 256);
   const size_t off_logit_part = off;
   off = round_up(off + kLogBlocks * sizeof(LogitPart), 256);
   const size_t off_logit_keys = off;
@@ -280,12 +285,12 @@ TLC_API int tlc_train_create(tlc_train** out, size_t max_tokens, size_t max_rows
                            sizeof(float), 256);
   e = hipMalloc(&c->ws, off);
   if (e == hipSuccess) e = hipMemset((uint8_t*)c->ws + off_touched, 0, max_rows);
-  if (e == hipSuccess) e = hipMemset((uint8_t*)c->ws + off_ticket, 0, 256);
+  if (e == hipSuccess) e = hipMemset((uint8_t*)c->ws + off_tickets, 0, kTicketBytes);
   if (e == hipSuccess) e = hipDeviceSynchronize();
   if (e == hipSuccess) e = hipHostMalloc((void**)&c->bad, 256, hipHostMallocDefault);
   if (e == hipSuccess) e = hipHostGetDevicePointer((void**)&c->bad_dev, c->bad, 0);
   if (e == hipSuccess && c->slot_pieces)
-    e = hipHostMalloc((void**)&c->staging, kGroups * kGroupSlots * c->slot_pieces * sizeof(Piece),
+    e = hipHostMalloc((void**)&c->staging, kGroups * kGroupSlots * c->slot_pieces * kSlotPiece,
                       hipHostMallocDefault);
   if (e == hipSuccess && c->staging)
     e = hipHostGetDevicePointer((void**)&c->staging_dev, c->staging, 0);
@@ -298,7 +303,7 @@ TLC_API int tlc_train_create(tlc_train** out, size_t max_tokens, size_t max_rows
   *c->bad = 0u;
   uint8_t* base = (uint8_t*)c->ws;
   c->partials = (double*)base;
-  c->ticket = (uint32_t*)(base + off_ticket);
+  c->tickets = (uint32_t*)(base + off_tickets);
   c->logit_part = (LogitPart*)(base + off_logit_part);
   c->logit_keys = (uint64_t*)(base + off_logit_keys);
   c->pieces = (Piece*)(base + off_pieces);
@@ -622,6 +627,7 @@ struct AdamCall {
   float* const* deltas;
   tlc_adamw_clock* clock;
   tlc_norm_result* result;
+  size_t total = 0;  // values; set by check_adamw
   bool small() const { return state_type == TLC_STATE_8BIT; }
 };
 
@@ -640,7 +646,48 @@ int check_options(const char* fn, const tlc_adamw_options* o, bool clips) {
   return TLC_OK;
 }
 
-int check_adamw(tlc_train* c, const char* fn, const AdamCall& l) {
+// f(kind, address, bytes, whether written) of every buffer of the call until one
+// returns false.
+constexpr int kSpanKinds = 8;
+template <class F>
+bool each_span(const AdamCall& l, F&& f) {
+  if (!f(0, l.clock, sizeof(*l.clock), true)) return false;
+  if (l.result && !f(1, l.result, sizeof(*l.result), true)) return false;
+  const size_t state = l.small() ? 1 : 4;
+  for (size_t i = 0; i < l.count; ++i) {
+    const size_t n = l.ns[i];
+    if (n == 0) continue;
+    const bool in_place = l.deltas && (const void*)l.deltas[i] == l.grads[i] &&
+                          l.grad_types[i] == TLC_F32;
+    if (!f(2, l.params[i], n * type_bytes(l.types[i]), true) ||
+        !f(3, l.grads[i], n * type_bytes(l.grad_types[i]), in_place) ||
+        !f(4, l.exp_avgs[i], n * state, true) || !f(5, l.exp_avg_sqs[i], n * state, true) ||
+        (l.small() && !f(6, l.scales[i], ceil_div(n, TLC_STATE_BLOCK) * 8, true)) ||
+        (l.deltas && !in_place && !f(7, l.deltas[i], n * 4, true)))
+      return false;
+  }
+  return true;
+}
+
+// Whether every kind of buffer rises in memory, as the tensors of one flat buffer
+// do, and no kind lies among another's: no overlap then, without a sort of all of
+// them (335 tensors whose addresses changed 19 us a call, 9 without).
+bool adam_runs_apart(const AdamCall& l) {
+  uintptr_t lo[kSpanKinds] = {}, hi[kSpanKinds] = {};
+  const bool rise = each_span(l, [&](int kind, const void* p, size_t bytes, bool) {
+    if (hi[kind] == 0) lo[kind] = (uintptr_t)p;
+    if ((uintptr_t)p < hi[kind]) return false;
+    hi[kind] = (uintptr_t)p + bytes;
+    return true;
+  });
+  if (!rise) return false;
+  for (int a = 0; a < kSpanKinds; ++a)
+    for (int b = 0; b < a; ++b)
+      if (lo[a] < hi[b] && lo[b] < hi[a]) return false;
+  return true;
+}
+
+int check_adamw(tlc_train* c, const char* fn, AdamCall& l) {
   if (!l.clock) return fail(TLC_E_INVALID, "%s: NULL clock", fn);
   if (l.state_type != TLC_STATE_F32 && l.state_type != TLC_STATE_8BIT)
     return fail(TLC_E_INVALID, "%s: unknown type of states %d", fn, l.state_type);
@@ -650,10 +697,6 @@ int check_adamw(tlc_train* c, const char* fn, const AdamCall& l) {
   if (l.count > c->max_tensors)
     return fail(TLC_E_INVALID, "%s: %zu tensors exceed the context's %zu", fn, l.count,
                 c->max_tensors);
-  c->spans.clear();
-  add_span(c->spans, l.clock, sizeof(*l.clock), true);
-  if (l.result) add_span(c->spans, l.result, sizeof(*l.result), true);
-  size_t total = 0;
   for (size_t i = 0; i < l.count; ++i) {
     const size_t n = l.ns[i];
     if (n == 0) continue;
@@ -665,22 +708,31 @@ int check_adamw(tlc_train* c, const char* fn, const AdamCall& l) {
     if (!l.params[i] || !l.grads[i] || !l.exp_avgs[i] || !l.exp_avg_sqs[i] ||
         (l.small() && !l.scales[i]) || (l.deltas && !l.deltas[i]))
       return fail(TLC_E_INVALID, "%s: tensor %zu: NULL pointer", fn, i);
-    total += n;
-    const size_t state = l.small() ? 1 : 4;
-    const bool in_place = l.deltas && (const void*)l.deltas[i] == l.grads[i] &&
-                          l.grad_types[i] == TLC_F32;
-    add_span(c->spans, l.params[i], n * type_bytes(l.types[i]), true);
-    add_span(c->spans, l.grads[i], n * type_bytes(l.grad_types[i]), in_place);
-    add_span(c->spans, l.exp_avgs[i], n * state, true);
-    add_span(c->spans, l.exp_avg_sqs[i], n * state, true);
-    if (l.small()) add_span(c->spans, l.scales[i], ceil_div(n, TLC_STATE_BLOCK) * 8, true);
-    if (l.deltas && !in_place) add_span(c->spans, l.deltas[i], n * 4, true);
+    l.total += n;
   }
-  if (total > kMaxListValues)
-    return fail(TLC_E_INVALID, "%s: %zu values exceed %zu", fn, total, kMaxListValues);
+  if (l.total > kMaxListValues)
+    return fail(TLC_E_INVALID, "%s: %zu values exceed %zu", fn, l.total, kMaxListValues);
+  if (adam_runs_apart(l)) return TLC_OK;
+  c->spans.clear();
+  each_span(l, [&](int, const void* p, size_t bytes, bool written) {
+    add_span(c->spans, p, bytes, written);
+    return true;
+  });
   if (spans_conflict_cached(c->spans, c->adamw_ok))
     return fail(TLC_E_INVALID, "%s: a written buffer overlaps another one", fn);
   return TLC_OK;
+}
+
+AdamTensor adam_tensor(const AdamCall& l, size_t i) {
+  AdamTensor e = {};
+  e.p = l.params[i];
+  e.g = l.grads[i];
+  e.m = l.exp_avgs[i];
+  e.v = l.exp_avg_sqs[i];
+  e.scales = l.small() ? l.scales[i] : nullptr;
+  e.delta = l.deltas ? l.deltas[i] : nullptr;
+  e.n = (uint32_t)l.ns[i];
+  return e;
 }
 
 // Tensors [first, next) of the call that have values, kAdamTensors at most.
@@ -690,21 +742,40 @@ AdamList adam_list(const AdamCall& l, size_t first, size_t* next) {
   for (; i < l.count && count < kAdamTensors; ++i)
     if (l.ns[i]) total += l.ns[i], ++count;
   *next = i;
-  r.len = piece_values(total, count);
+  r.len = adam_piece_values(total, count, kAdamUnit);
+  r.state_bytes = l.small() ? 1 : 4;
   for (i = first; i < *next; ++i) {
     if (l.ns[i] == 0) continue;
-    AdamTensor& e = r.tensors[r.count++];
-    e.p = l.params[i];
-    e.g = l.grads[i];
-    e.m = l.exp_avgs[i];
-    e.v = l.exp_avg_sqs[i];
-    e.scales = l.small() ? l.scales[i] : nullptr;
-    e.delta = l.deltas ? l.deltas[i] : nullptr;
-    e.n = (uint32_t)l.ns[i];
+    AdamTensor& e = r.tensors[r.count++] = adam_tensor(l, i);
     e.piece0_types = r.n | (uint32_t)l.types[i] << 28 | (uint32_t)l.grad_types[i] << 30;
     r.n += (uint32_t)ceil_div(l.ns[i], r.len);
   }
   return r;
+}
+
+AdamPinned adam_pinned(const AdamCall& l, size_t total, AdamPiece* host, const AdamPiece* dev) {
+  AdamPinned r = {dev, 0};
+  const size_t len = adam_piece_values(total, l.count, 2 * kAdamUnit);
+  for (size_t i = 0; i < l.count; ++i) {
+    const AdamTensor e = adam_tensor(l, i);
+    const uint32_t types = (uint32_t)l.types[i] | (uint32_t)l.grad_types[i] << 2;
+    for (size_t k = 0; k < l.ns[i]; k += len)
+      host[r.n++] = adam_piece(e, types, (uint32_t)k, (uint32_t)len, l.small() ? 1 : 4);
+  }
+  return r;
+}
+
+// Whether the call's tensors take more than one launch's arguments, and the
+// stream is not being captured (a replay would read a slot that later calls have
+// filled again: it has several launches).
+int pins(tlc_train* c, size_t tensors, bool* yes) {
+  *yes = false;
+  if (tensors <= kAdamTensors) return TLC_OK;
+  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+  const hipError_t e = hipStreamIsCapturing(c->stream, &capture);
+  if (e != hipSuccess) return hip_fail(e, "hipStreamIsCapturing");
+  *yes = capture == hipStreamCaptureStatusNone && c->slot_pieces;
+  return TLC_OK;
 }
 
 }  // namespace
@@ -718,8 +789,8 @@ TLC_API int tlc_adamw(tlc_train* c, size_t count, void* const* params, const int
   const char* fn = "tlc_adamw";
   int st = check_usable(c, fn);
   if (st) return st;
-  const AdamCall l{count,       params, types,  ns,    grads, grad_types, state_type, exp_avgs,
-                   exp_avg_sqs, scales, deltas, clock, result};
+  AdamCall l{count,       params, types,  ns,    grads, grad_types, state_type, exp_avgs,
+             exp_avg_sqs, scales, deltas, clock, result};
   st = check_options(fn, options, result != nullptr);
   if (!st) st = check_adamw(c, fn, l);
   if (st) return st;
@@ -737,10 +808,23 @@ TLC_API int tlc_adamw(tlc_train* c, size_t count, void* const* params, const int
   a.max_norm = options->max_norm;
   a.clock = clock;
   a.result = result;
+  bool pinned = false;
+  st = pins(c, count, &pinned);
+  if (st) return st;
+  if (pinned) {
+    AdamPiece* host = nullptr;
+    const AdamPiece* pieces = nullptr;
+    st = take_slot(c, &host, &pieces);
+    if (st) return st;
+    a.tickets = c->tickets;
+    st = launched(c, launch_adamw(adam_pinned(l, l.total, host, pieces), a, state_type, c->stream),
+                  fn);
+    return st ? st : leave_slot(c);
+  }
   size_t next = 0;
   do {
     const AdamList list = adam_list(l, next, &next);
-    a.ticket = next >= count ? c->ticket : nullptr;
+    a.tickets = next >= count ? c->tickets : nullptr;
     st = launched(c, launch_adamw(list, a, state_type, c->stream), fn);
   } while (!st && next < count);
   return st;

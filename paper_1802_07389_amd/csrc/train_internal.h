@@ -259,6 +259,17 @@ hipError_t launch_token_grad(const TokenGradArgs& a, int type, int out_type, hip
 // ---- AdamW
 constexpr uint32_t kAdamThreads = 256;
 constexpr uint32_t kAdamTensors = 64;  // of a launch
+// Pieces, about kNormBlocks of them at most as in a list of the norm, are multiples
+// of kAdamUnit values, four a thread, so that few values still fill the chip
+// (1000003 of 8 bits 8.0 us, in pieces of 4096 9.8); in pinned memory of twice as
+// many, as a piece takes 3 ns of the bus (335 tensors of 1.7M values 16.4 | 18.8 us
+// with 2048 | 1024).
+constexpr uint32_t kAdamUnit = 1024;
+inline uint32_t adam_piece_values(size_t total, size_t count, uint32_t unit) {
+  const size_t most = kNormBlocks - std::min<size_t>(count, kNormBlocks / 2);
+  const size_t units = (total + most * unit - 1) / (most * unit);
+  return (uint32_t)(std::max<size_t>(units, 1) * unit);
+}
 struct AdamTensor {
   void* p;
   const void* g;
@@ -272,7 +283,41 @@ struct AdamTensor {
 struct AdamList {
   uint32_t count, n;  // tensors, pieces
   uint32_t len;       // values of a piece
+  uint32_t state_bytes;  // of a value of m or v
   AdamTensor tensors[kAdamTensors];
+};
+// A piece with pointers to its values, which begin at value k0 of their tensor.
+struct AdamPiece {
+  void* p;
+  const void* g;
+  void* m;
+  void* v;
+  float* scales;
+  float* delta;
+  uint32_t n, k0;
+  uint32_t types;  // p's in bits 0 and 1, g's in 2 and 3
+  uint32_t reserved;
+};
+static_assert(sizeof(AdamPiece) == 64, "AdamPiece is 64 bytes");
+__host__ __device__ inline AdamPiece adam_piece(const AdamTensor& t, uint32_t types, uint32_t k0,
+                                                uint32_t len, uint32_t state_bytes) {
+  AdamPiece r;
+  r.p = (uint8_t*)t.p + (uint64_t)k0 * ((types & 3u) == TLC_F32 ? 4 : 2);
+  r.g = (const uint8_t*)t.g + (uint64_t)k0 * ((types >> 2) == TLC_F32 ? 4 : 2);
+  r.m = (uint8_t*)t.m + (uint64_t)k0 * state_bytes;
+  r.v = (uint8_t*)t.v + (uint64_t)k0 * state_bytes;
+  r.scales = t.scales ? t.scales + k0 / TLC_STATE_BLOCK * 2 : nullptr;
+  r.delta = t.delta ? t.delta + k0 : nullptr;
+  r.n = len < t.n - k0 ? len : t.n - k0;
+  r.k0 = k0;
+  r.types = types;
+  r.reserved = 0u;
+  return r;
+}
+// More tensors than a launch's arguments hold: their pieces in pinned host memory.
+struct AdamPinned {
+  const AdamPiece* pieces;
+  uint32_t n;
 };
 struct AdamArgs {
   double lr, log_beta1, log_beta2, decay;
@@ -280,9 +325,14 @@ struct AdamArgs {
   float eps, max_norm;
   tlc_adamw_clock* clock;
   tlc_norm_result* result;  // NULL: no clipping
-  uint32_t* ticket;         // the step's last launch: counts its blocks; else NULL
+  uint32_t* tickets;        // the step's last launch: counts its blocks; else NULL
 };
+// The counters: of the groups, and of each group's blocks, each in a cache line
+// of its own; zero between calls.
+constexpr uint32_t kTicketGroups = 64, kTicketWords = 32;
+constexpr size_t kTicketBytes = (1 + kTicketGroups) * kTicketWords * sizeof(uint32_t);
 static_assert(sizeof(AdamList) + sizeof(AdamArgs) <= 3840, "kernel arguments end at 4096 bytes");
-hipError_t launch_adamw(const AdamList& list, const AdamArgs& a, int state_type, hipStream_t st);
+template <class List>
+hipError_t launch_adamw(const List& list, const AdamArgs& a, int state_type, hipStream_t st);
 
 }  // namespace tlc
