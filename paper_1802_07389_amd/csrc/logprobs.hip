@@ -8,6 +8,8 @@
 #include <float.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "device_common.hpp"
 #include "train_internal.h"
 #include "typed_io.hpp"
@@ -19,6 +21,7 @@ constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 // Exponents are clamped here where they multiply a probability of 0: a logit of
 // -inf adds 0 * kFar and not 0 * -inf.
 constexpr float kFar = -1e30f;
+constexpr float kFarRef = 65536.0f;  // m c below it, which fp32 rounds by 2^-8 at most
 
 // A row's target: its column, kNoTarget where the call has none, kLeftOut where
 // it is the ignored id or outside the vocabulary.
@@ -48,10 +51,17 @@ __device__ __forceinline__ LogitPart merged(LogitPart a, LogitPart b, float c) {
   return LogitPart{m, a.s0 + b.s0, a.s1 + b.s1};
 }
 
-constexpr int kLogWaves = kLogThreads / 64;
+// The larger of three.  (fmaxf() has the compiler quiet every operand first: two
+// instructions more a value.)  NaN may get lost here; the sums keep it.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
 
-// Of a whole block, the same in every thread.  Uses lds[kLogWaves] and one
+// Of a whole block, the same in every thread.  Uses lds[kThreads / 64] and one
 // barrier.
+template <int kThreads>
 __device__ __forceinline__ LogitPart block_merged(LogitPart p, float c, LogitPart* lds) {
   float m = p.m;
 #pragma unroll
@@ -62,11 +72,12 @@ __device__ __forceinline__ LogitPart block_merged(LogitPart p, float c, LogitPar
     p.s0 += __shfl_xor(p.s0, d);
     p.s1 += __shfl_xor(p.s1, d);
   }
+  if constexpr (kThreads == 64) return p;
   if ((threadIdx.x & 63u) == 0) lds[threadIdx.x >> 6] = p;
   __syncthreads();
   LogitPart r = lds[0];
 #pragma unroll
-  for (int w = 1; w < kLogWaves; ++w) r = merged(r, lds[w], c);
+  for (int w = 1; w < kThreads / 64; ++w) r = merged(r, lds[w], c);
   return r;
 }
 
@@ -79,17 +90,6 @@ struct RowPacks {
   uint32_t vocab;
   __device__ __forceinline__ uint32_t start(uint32_t p) const {
     return umin32(p * V, vocab - V);
-  }
-  // Pack p with the columns that are not its own set to -inf; all of them where
-  // p >= end.
-  __device__ __forceinline__ Pack<T, V> load(uint32_t p, uint32_t end) const {
-    const uint32_t q = umin32(p, end - 1), k = start(q);
-    Pack<T, V> r = load_pack<T, V>(x + k);
-    const uint32_t skip = p < end ? q * V - k : V;
-#pragma unroll
-    for (int e = 0; e < V; ++e)
-      if ((uint32_t)e < skip) r.set(e, -INFINITY);
-    return r;
   }
 };
 
@@ -105,32 +105,41 @@ __device__ __forceinline__ float key_logit(uint64_t key) {
   return __uint_as_float((order >> 31) ? order & 0x7fffffffu : ~order);
 }
 
-// The block's selection of the largest keys.
-constexpr uint32_t kFewKeys = kLogThreads;
+// The block's selection of the largest keys: rounds of kRoundKeys a thread at
+// most, after kFewKeys at most.  (16.9 KB of 256 threads: nine blocks a CU.)
+constexpr uint32_t kFewKeys = 256, kRoundKeys = 4;
+// Parts whose segments are looked at together; a wave's rows have one.
+template <int kThreads>
+constexpr uint32_t kLiveParts = kThreads == 64 ? 1 : 8;
+template <int kThreads>
 struct TopLds {
-  uint64_t keys[kLogThreads];
-  uint64_t found[kFewKeys + kLogThreads * 8];
+  uint64_t keys[kThreads];
+  uint64_t found[kFewKeys + kThreads * kRoundKeys];
   uint64_t best[TLC_MAX_TOP];
-  uint64_t least;  // found keys below it are not among the largest
-  uint32_t from[TLC_MAX_TOP];
-  uint32_t count;
+  uint16_t live[kThreads * kLiveParts<kThreads>];  // part * kThreads + thread, of 256 parts at most
+  uint64_t least;
+  uint32_t found_count, live_count;
 };
 
 // How many of keys[0, n) are above `key`.
 __device__ __forceinline__ uint32_t rank_of(const uint64_t* keys, uint32_t n, uint64_t key) {
-  uint32_t r = 0;
-  for (uint32_t j = 0; j < n; ++j) r += keys[j] > key;
+  uint32_t r = 0, j = 0;
+  for (; j + 8 <= n; j += 8) {
+    uint64_t k[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) k[i] = keys[j + i];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r += k[i] > key;
+  }
+  for (; j < n; ++j) r += keys[j] > key;
   return r;
 }
 
-__device__ __forceinline__ void put_key(TopLds& l, uint64_t key) {
-  if (key >= l.least) l.found[atomicAdd(&l.count, 1u)] = key;
-}
-
-// best: the `top` largest of the found keys, in order; they stay as the found
+// best: the `top` largest of the n found keys, in order; they stay as the found
 // ones.  All threads; begins after a barrier and ends with one.
-__device__ __forceinline__ void keep_best(TopLds& l, uint32_t n, uint32_t top) {
-  for (uint32_t j = threadIdx.x; j < n; j += kLogThreads) {
+template <int kThreads>
+__device__ __forceinline__ void keep_best(TopLds<kThreads>& l, uint32_t n, uint32_t top) {
+  for (uint32_t j = threadIdx.x; j < n; j += kThreads) {
     const uint64_t key = l.found[j];
     const uint32_t r = rank_of(l.found, n, key);
     if (r < top) l.best[r] = key;
@@ -138,19 +147,8 @@ __device__ __forceinline__ void keep_best(TopLds& l, uint32_t n, uint32_t top) {
   __syncthreads();
   const uint32_t kept = umin32(n, top);
   if (threadIdx.x < kept) l.found[threadIdx.x] = l.best[threadIdx.x];
-  if (threadIdx.x == 0) {
-    l.count = kept;
-    if (n >= top) l.least = l.best[top - 1];
-  }
+  if (threadIdx.x == 0) l.found_count = kept;
   __syncthreads();
-}
-
-// After a round that adds at most eight keys a thread.
-__device__ __forceinline__ void end_round(TopLds& l, uint32_t top) {
-  __syncthreads();
-  const uint32_t n = l.count;
-  __syncthreads();
-  if (n > kFewKeys) keep_best(l, n, top);
 }
 
 // The row's statistics from the merged sums.
@@ -181,8 +179,11 @@ __device__ __forceinline__ void put_left_out(const TokenArgs& a, uint32_t row) {
   }
 }
 
-__device__ __forceinline__ void put_top(const TokenArgs& a, uint32_t row, const uint64_t* best,
-                                        const tlc_token_result& r) {
+// A row's results, with its best keys in LDS.
+__device__ __forceinline__ void put_row(const TokenArgs& a, uint32_t row, LogitPart sum,
+                                        int64_t target, float x, const uint64_t* best) {
+  const tlc_token_result r = result_of(sum, a.scale, target >= 0, x);
+  if (threadIdx.x == 0) a.results[row] = r;
   if (threadIdx.x >= a.top) return;
   const uint64_t at = (uint64_t)row * a.top + threadIdx.x;
   if (r.max != r.max) {
@@ -196,191 +197,279 @@ __device__ __forceinline__ void put_top(const TokenArgs& a, uint32_t row, const 
   a.top_ids[at] = (int32_t)~(uint32_t)key;
 }
 
-constexpr uint32_t kLogUnits = 4;  // packs of a thread in flight
-constexpr uint32_t kLogChunk = kLogThreads * kLogUnits;
 
 struct Lane {
   LogitPart p;
-  float best;      // largest logit of the thread, and the chunk that had it first
-  uint32_t chunk;
+  float best;     // largest logit of the thread, and the pack that had it first
+  uint32_t pack;
 };
 
-template <class T, int V, bool kTop>
-__device__ __forceinline__ void add_chunk(Lane& l, const Pack<T, V> (&r)[kLogUnits], float c,
-                                          uint32_t chunk) {
-  float mx = r[0].get(0);
+// Packs first, first + kThreads, ... of a thread, kUnits of them; of a masked one
+// the first `skip` columns are not its own (V: none is).
+//
+// Exponents are one fused x c - R, by R = m c rounded, and the sums are corrected
+// for R - m c once: a value takes its conversion, half a maximum, a multiply-add,
+// 2^t (a quarter of the others' rate), an addition and a multiply-add, which is what
+// bounds large calls.  Where an exponent is not finite (masked entries, or what is
+// NaN in the end) or R so large that the correction is, the wave takes the sums
+// again with differences of x and m: no chunk of 4 packs pays for it before it
+// holds such a value.
+template <class T, int V, bool kTop, int kThreads, bool kMasked, uint32_t kUnits>
+__device__ __forceinline__ void add_packs(Lane& l, const Pack<T, V> (&r)[kUnits], float c,
+                                          uint32_t first, uint32_t skip) {
+  if (kMasked && skip >= V) return;
+  const auto own = [&](int e) { return !kMasked || (uint32_t)e >= skip; };
+  const auto seen = [&](uint32_t u, int e) { return own(e) ? r[u].get(e) : -INFINITY; };
+  float most = -INFINITY;
 #pragma unroll
-  for (uint32_t u = 0; u < kLogUnits; ++u)
+  for (uint32_t u = 0; u < kUnits; ++u) {
+    float pm = seen(u, 0);
 #pragma unroll
-    for (int e = 0; e < V; ++e) mx = fmaxf(mx, r[u].get(e));
-  if (kTop && mx > l.best) {
-    l.best = mx;
-    l.chunk = chunk;
+    for (int e = 1; e < V; e += 2) pm = max3(pm, seen(u, e), seen(u, e + 1 < V ? e + 1 : e));
+    if (kTop && pm > l.best) {
+      l.best = pm;
+      l.pack = first + u * kThreads;
+    }
+    most = max3(most, pm, pm);
   }
-  l.p = rebased(l.p, fmaxf(l.p.m, mx), c);
+  if (__ballot(most != -INFINITY) == 0) {  // masked entries add nothing; but NaN is no maximum
+    bool only = true;
 #pragma unroll
-  for (uint32_t u = 0; u < kLogUnits; ++u)
+    for (uint32_t u = 0; u < kUnits; ++u)
+#pragma unroll
+      for (int e = 0; e < V; ++e) only &= !own(e) || r[u].get(e) == -INFINITY;
+    if (__ballot(!only) == 0) return;
+  }
+  const float m = fmaxf(l.p.m, most), ref = m * c;
+  float d = __builtin_fmaf(-m, c, ref), s0 = 0.0f, s1 = 0.0f;
+#pragma unroll
+  for (uint32_t u = 0; u < kUnits; ++u)
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      const float t = (r[u].get(e) - l.p.m) * c, w = exp2_of(t);
-      l.p.s0 += w;
-      l.p.s1 = __builtin_fmaf(w, fmaxf(t, kFar), l.p.s1);
+      const float t = own(e) ? __builtin_fmaf(r[u].get(e), c, -ref) : kFar, w = exp2_of(t);
+      s0 += w;
+      s1 = __builtin_fmaf(w, t, s1);
     }
+  if (__ballot(!(s1 == s1 && fabsf(ref) < kFarRef)) != 0) {
+    d = s0 = s1 = 0.0f;
+#pragma unroll
+    for (uint32_t u = 0; u < kUnits; ++u)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float t = own(e) ? (r[u].get(e) - m) * c : kFar, w = exp2_of(t);
+        s0 += w;
+        s1 = __builtin_fmaf(w, fmaxf(t, kFar), s1);
+      }
+  }
+  const float f = exp2_of(d);
+  l.p = rebased(l.p, m, c);
+  l.p.s0 += f * s0;
+  l.p.s1 += f * (s1 + d * s0);
 }
 
-// The `top` largest keys of packs [p0, p0 + n) into lds.best (fewer where there
-// are fewer columns: lds.count).  A thread's columns hold one of them only if the
-// thread's largest is among the `top` largest of all threads', so that `top` threads'
-// columns are read again, and of them the keys from the least of those on are
-// ranked.
-template <class T, int V>
-__device__ __forceinline__ void select_top(const RowPacks<T, V>& row, uint32_t p0, uint32_t n,
-                                           const Lane& l, uint32_t top, TopLds& lds) {
-  const uint32_t tid = threadIdx.x, end = p0 + n;
+// A segment: the columns of one thread of one part; its key is that of its
+// largest logit, with the pack that had it first in the column's place (0: no
+// columns).  own: the keys of this thread's segments of the first kLiveParts<kThreads> parts;
+// seg(j, own) those of the parts from j on.
+//
+// The `top` largest keys of the row's columns into lds.best.  Groups of segments
+// (four neighbouring threads' where `top` is small beside 64, else a thread's)
+// have their largest keys ranked.  The top-th of these is the key of a column, so a column
+// below it is not among the `top` largest, and a segment below it has none of them:
+// the others' columns are read again, about `top` of them.
+template <class T, int V, int kThreads, class Seg>
+__device__ __forceinline__ void select_top(const RowPacks<T, V>& row, const TokenArgs& a,
+                                           uint32_t packs, uint64_t (&own)[kLiveParts<kThreads>],
+                                           Seg&& seg, TopLds<kThreads>& lds) {
+  const uint32_t tid = threadIdx.x, top = a.top;
+  const bool quads = kThreads > 64 && top <= kQuadTop;
   uint64_t key = 0;
-  if (tid < n) {
-    uint32_t at = ~0u;
+  for (uint32_t j0 = 0; j0 < a.parts; j0 += kLiveParts<kThreads>) {
+    if (j0 > 0) seg(j0, own);
 #pragma unroll
-    for (uint32_t u = kLogUnits; u-- > 0;) {
-      const uint32_t p = p0 + l.chunk * kLogChunk + u * kLogThreads + tid;
-      const Pack<T, V> r = row.load(p, end);
-      const uint32_t k = row.start(umin32(p, end - 1));
-#pragma unroll
-      for (int e = V - 1; e >= 0; --e)
-        if (p < end && k + e >= p * V && r.get(e) == l.best) at = k + e;
-    }
-    key = key_of(l.best, at);
+    for (uint32_t j = 0; j < kLiveParts<kThreads>; ++j) key = own[j] > key ? own[j] : key;
   }
-  lds.keys[tid] = key;
+  if (quads) {
+#pragma unroll
+    for (int d = 1; d < 4; d <<= 1) {
+      const uint64_t k = __shfl_xor(key, d);
+      key = k > key ? k : key;
+    }
+    if ((tid & 3u) == 0) lds.keys[tid >> 2] = key;
+  } else {
+    lds.keys[tid] = key;
+  }
   if (tid == 0) {
-    lds.count = 0;
+    lds.found_count = lds.live_count = 0;
     lds.least = 0;
   }
   __syncthreads();
-  const uint32_t threads = umin32(umin32(n, kLogThreads), top);
-  const uint32_t r = rank_of(lds.keys, kLogThreads, key);
-  if (key != 0 && r < threads) {
-    lds.from[r] = tid;
-    if (r == top - 1) lds.least = key;
+  // the top-th largest key; 0 where there are fewer
+  uint64_t least;
+  if (kThreads == 64 || quads) {  // every wave for itself
+    const uint64_t k = lds.keys[tid & 63u];
+    const uint64_t who = __ballot(k != 0 && rank_of(lds.keys, 64, k) == top - 1);
+    const int lane = __ffsll((unsigned long long)who) - 1;
+    least = who == 0 ? 0
+                     : (uint64_t)(uint32_t)__shfl((int)(uint32_t)k, lane) |
+                           (uint64_t)(uint32_t)__shfl((int)(uint32_t)(k >> 32), lane) << 32;
+  } else {
+    if (key != 0 && rank_of(lds.keys, kThreads, key) == top - 1) lds.least = key;
+    __syncthreads();
+    least = lds.least;
   }
-  __syncthreads();
-  const uint32_t each = (n + kLogThreads - 1) / kLogThreads;  // packs of a thread
-  for (uint32_t w0 = 0; w0 < threads * each; w0 += kLogThreads) {
-    const uint32_t w = w0 + tid, s = w / each;
-    const uint32_t i = s < threads ? lds.from[s] + (w - s * each) * kLogThreads : n;
-    if (i < n) {
-      const uint32_t p = p0 + i, k = row.start(p);
-      const Pack<T, V> x = load_pack<T, V>(row.x + k);
+  // the same as a column's key, of the last column that its pack may have
+  const uint64_t floor =
+      least == 0 ? 0 : (least >> 32 << 32) | (uint32_t)~(~(uint32_t)least * V + (V - 1));
+  const uint32_t each = (a.part_packs + kThreads - 1) / kThreads;  // packs of a segment
+  for (uint32_t j0 = 0; j0 < a.parts; j0 += kLiveParts<kThreads>) {
+    if (a.parts > kLiveParts<kThreads>) seg(j0, own);
 #pragma unroll
-      for (int e = 0; e < V; ++e)
-        if (k + e >= p * V) put_key(lds, key_of(x.get(e), k + e));
+    for (uint32_t j = 0; j < kLiveParts<kThreads>; ++j)
+      if (own[j] != 0 && own[j] >= least)
+        lds.live[atomicAdd(&lds.live_count, 1u)] = (uint16_t)((j0 + j) * kThreads + tid);
+    __syncthreads();
+    const uint32_t items = lds.live_count * each;
+    for (uint32_t w0 = 0; w0 < items; w0 += kThreads) {
+      const uint32_t w = w0 + tid;
+      uint32_t p = packs, k = 0;
+      Pack<T, V> x = {};
+      if (w < items) {
+        const uint32_t s = w / each, part = lds.live[s] / kThreads;
+        const uint32_t i = lds.live[s] - part * kThreads + (w - s * each) * kThreads;
+        if (i < a.part_packs) p = part * a.part_packs + i;
+        if (p < packs) {
+          k = row.start(p);
+          x = load_pack<T, V>(row.x + k);
+        }
+      }
+#pragma unroll
+      for (int e0 = 0; e0 < V; e0 += kRoundKeys) {
+        if (p < packs)
+#pragma unroll
+          for (int e = e0; e < V && e < e0 + (int)kRoundKeys; ++e) {
+            const uint64_t c = key_of(x.get(e), k + e);
+            if (k + e >= p * V && c >= floor) lds.found[atomicAdd(&lds.found_count, 1u)] = c;
+          }
+        __syncthreads();
+        const uint32_t n = lds.found_count;
+        __syncthreads();
+        if (n > kFewKeys) keep_best(lds, n, top);
+      }
     }
-    end_round(lds, top);
+    if (tid == 0) lds.live_count = 0;
+    __syncthreads();
   }
-  keep_best(lds, lds.count, top);
+  keep_best(lds, lds.found_count, top);
+}
+
+// Stores and loads of what blocks hand to one another: they go to where all of the
+// card's caches meet, so that a block which has waited for its stores may count
+// itself as done without a fence (a fence writes back a whole L2: 16 ns a block,
+// one after the other; 64 rows of 131072 fp32 values in 512 blocks 14.4 us).
+template <class W>
+__device__ __forceinline__ void hand_over(W* p, W v) {
+  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <class W>
+__device__ __forceinline__ W take_over(const W* p) {
+  return __hip_atomic_load(const_cast<W*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 }  // namespace
 
-// A block reads a row, or one of `parts` parts of it, whose sums and keys
-// tlc_token_join_kernel puts together.
-template <class T, int V, bool kTop>
-__global__ __launch_bounds__(kLogThreads) void tlc_token_logprobs_kernel(TokenArgs a) {
-  __shared__ LogitPart sums[kLogWaves];
-  __shared__ TopLds lds;
+// A block reads a row, or one of `parts` parts of it; the last of a row's blocks
+// puts the parts together.
+template <class T, int V, bool kTop, int kThreads, uint32_t kUnits, bool kStream>
+__global__ __launch_bounds__(kThreads) void tlc_token_logprobs_kernel(TokenArgs a) {
+  constexpr uint32_t kChunk = kThreads * kUnits;
+  __shared__ LogitPart sums[kThreads / 64];
+  __shared__ std::conditional_t<kTop, TopLds<kThreads>, uint64_t> lds;
+  __shared__ uint32_t last;
   const uint32_t packs = (a.vocab + V - 1) / V, full = a.vocab / V;
   const float c = a.scale * kLog2e;
   const uint64_t blocks = (uint64_t)a.count * a.parts;
   for (uint64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
     const uint32_t row = (uint32_t)(b / a.parts), part = (uint32_t)(b - (uint64_t)row * a.parts);
-    const int64_t target = target_of(a, row, a.parts == 1 && threadIdx.x == 0);
+    const int64_t target = target_of(a, row, part == 0 && threadIdx.x == 0);
     if (target == kLeftOut) {
-      if (a.parts == 1) put_left_out(a, row);
+      if (part == 0) put_left_out(a, row);
       continue;
     }
     const RowPacks<T, V> xs{static_cast<const T*>(a.x) + row * a.stride, a.vocab};
     const uint32_t p0 = part * a.part_packs, end = umin32(p0 + a.part_packs, packs);
     const float x = target >= 0 ? (float)xs.x[target] : 0.0f;
-    Lane l{{-FLT_MAX, 0.0f, 0.0f}, -INFINITY, 0u};
-    const uint32_t n = end - p0, whole = (umin32(end, full) - p0) / kLogChunk;
+    Lane l{{-FLT_MAX, 0.0f, 0.0f}, -INFINITY, p0 + threadIdx.x};
+    const uint32_t n = end - p0, own_full = umin32(end, full) - p0;
     uint32_t i = 0;
-    Pack<T, V> r[kLogUnits];
-    for (; i < whole; ++i) {
+    for (; i + kChunk <= own_full; i += kChunk) {
+      const uint32_t p = p0 + i + threadIdx.x;
+      Pack<T, V> r[kUnits];
 #pragma unroll
-      for (uint32_t u = 0; u < kLogUnits; ++u)
-        r[u] = load_pack<T, V>(
-            xs.x + (p0 + i * kLogChunk + u * kLogThreads + threadIdx.x) * V);
-      add_chunk<T, V, kTop>(l, r, c, i);
+      for (uint32_t u = 0; u < kUnits; ++u)
+        r[u] = load_pack<T, V, kStream>(xs.x + (p + u * kThreads) * V);
+      add_packs<T, V, kTop, kThreads, false>(l, r, c, p, 0);
     }
-    for (; i * kLogChunk < n; ++i) {
+    if (i < n) {  // packs of the last columns, asked for before any is taken
+      const uint32_t p = p0 + i + threadIdx.x;
+      Pack<T, V> r[kUnits][1];
 #pragma unroll
-      for (uint32_t u = 0; u < kLogUnits; ++u)
-        r[u] = xs.load(p0 + i * kLogChunk + u * kLogThreads + threadIdx.x, end);
-      add_chunk<T, V, kTop>(l, r, c, i);
-    }
-    const LogitPart sum = block_merged(l.p, c, sums);
-    const bool ordered = sum.s0 >= 0.0f;  // no NaN
-    if (kTop && ordered) select_top(xs, p0, n, l, a.top, lds);
-    if (a.parts == 1) {
-      const tlc_token_result res = result_of(sum, a.scale, target >= 0, x);
-      if (threadIdx.x == 0) a.results[row] = res;
-      if (kTop) put_top(a, row, lds.best, res);
-    } else {
-      if (threadIdx.x == 0) a.part[b] = sum;
-      if (kTop && threadIdx.x < a.top)
-        a.keys[b * a.top + threadIdx.x] =
-            ordered && threadIdx.x < lds.count ? lds.best[threadIdx.x] : 0;
-    }
-    __syncthreads();
-  }
-}
-
-// The parts of a row put together, a block each.
-template <class T>
-__global__ __launch_bounds__(kLogThreads) void tlc_token_join_kernel(TokenArgs a) {
-  __shared__ LogitPart sums[kLogWaves];
-  __shared__ TopLds lds;
-  const uint32_t row = blockIdx.x, tid = threadIdx.x;
-  const int64_t target = target_of(a, row, tid == 0);
-  if (target == kLeftOut) {
-    put_left_out(a, row);
-    return;
-  }
-  const uint64_t first = (uint64_t)row * a.parts;
-  const float c = a.scale * kLog2e;
-  const float x = target >= 0 ? (float)(static_cast<const T*>(a.x) + row * a.stride)[target] : 0.0f;
-  LogitPart p{-FLT_MAX, 0.0f, 0.0f};
-  if (tid < a.parts) p = a.part[first + tid];
-  const LogitPart sum = block_merged(p, c, sums);
-  const tlc_token_result res = result_of(sum, a.scale, target >= 0, x);
-  if (tid == 0) a.results[row] = res;
-  if (a.top == 0) return;
-  if (sum.s0 >= 0.0f) {
-    // the first `deep` keys of `lists` parts are `top` keys or more, none below the
-    // least of their deep-th ones
-    const uint32_t deep = (a.top + a.parts - 1) / a.parts, lists = (a.top + deep - 1) / deep;
-    const uint64_t* keys = a.keys + first * a.top;
-    const uint64_t key = tid < a.parts ? keys[tid * a.top + deep - 1] : 0;
-    lds.keys[tid] = key;
-    if (tid == 0) {
-      lds.count = 0;
-      lds.least = 1;  // 0: no key
-    }
-    __syncthreads();
-    if (key != 0 && rank_of(lds.keys, a.parts, key) == lists - 1) lds.least = key;
-    __syncthreads();
-    const uint32_t n = a.parts * a.top;
-    for (uint32_t i0 = 0; i0 < n; i0 += kLogThreads * 8) {
+      for (uint32_t u = 0; u < kUnits; ++u)
+        r[u][0] = load_pack<T, V>(xs.x + xs.start(umin32(p + u * kThreads, end - 1)));
 #pragma unroll
-      for (uint32_t u = 0; u < 8; ++u) {
-        const uint32_t i = i0 + u * kLogThreads + tid;
-        if (i < n) put_key(lds, keys[i]);
+      for (uint32_t u = 0; u < kUnits; ++u) {
+        const uint32_t q = p + u * kThreads;
+        if (i + (u + 1) * kThreads <= own_full)
+          add_packs<T, V, kTop, kThreads, false>(l, r[u], c, q, 0);
+        else if (i + u * kThreads < n)
+          add_packs<T, V, kTop, kThreads, true>(l, r[u], c, q,
+                                                q < end ? q * V - xs.start(q) : V);
       }
-      end_round(lds, a.top);
     }
-    keep_best(lds, lds.count, a.top);
+    LogitPart sum = block_merged<kThreads>(l.p, c, sums);
+    const uint64_t key = threadIdx.x < n ? key_of(l.best, l.pack) : 0;
+    const uint64_t first = (uint64_t)row * a.parts;
+    const uint64_t* const keys = a.keys + first * kThreads + threadIdx.x;
+    const auto seg = [&](uint32_t j0, uint64_t(&own)[kLiveParts<kThreads>]) {
+#pragma unroll
+      for (uint32_t j = 0; j < kLiveParts<kThreads>; ++j)
+        own[j] = take_over(keys + umin32(j0 + j, a.parts - 1) * kThreads);
+#pragma unroll
+      for (uint32_t j = 0; j < kLiveParts<kThreads>; ++j)
+        if (j0 + j >= a.parts) own[j] = 0;
+    };
+    uint64_t own[kLiveParts<kThreads>] = {key};
+    if (a.parts > 1) {
+      if (threadIdx.x == 0) {
+        hand_over(&a.part[b].m, sum.m);
+        hand_over(&a.part[b].s0, sum.s0);
+        hand_over(&a.part[b].s1, sum.s1);
+      }
+      if (kTop) hand_over(a.keys + b * kThreads + threadIdx.x, key);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      if (threadIdx.x == 0)
+        last = __hip_atomic_fetch_add(a.tickets + row * kTicketWords, 1u, __ATOMIC_RELAXED,
+                                      __HIP_MEMORY_SCOPE_AGENT) == a.parts - 1;
+      __syncthreads();
+      if (!last) continue;
+      if (threadIdx.x == 0) a.tickets[row * kTicketWords] = 0u;
+      if (kTop) seg(0, own);
+      LogitPart p{-FLT_MAX, 0.0f, 0.0f};
+      for (uint32_t j = threadIdx.x; j < a.parts; j += kThreads) {
+        const LogitPart* q = a.part + first + j;
+        p = merged(p, LogitPart{take_over(&q->m), take_over(&q->s0), take_over(&q->s1)}, c);
+      }
+      sum = block_merged<kThreads>(p, c, sums);
+    }
+    if constexpr (kTop)
+      if (sum.s0 >= 0.0f) select_top(xs, a, packs, own, seg, lds);  // no NaN
+    if constexpr (kTop)
+      put_row(a, row, sum, target, x, lds.best);
+    else
+      put_row(a, row, sum, target, x, nullptr);
+    __syncthreads();
   }
-  put_top(a, row, lds.best, res);
 }
 
 // The gradient, kGradUnits packs of a row a thread; rows that are left out, or
@@ -438,29 +527,34 @@ namespace {
 
 constexpr uint64_t kMostBlocks = 1u << 22;
 
-template <class T, int V>
-hipError_t logprobs_packs(const TokenArgs& a, hipStream_t st) {
-  const uint64_t blocks = std::min((uint64_t)a.count * a.parts, kMostBlocks);
+
+template <class T, int V, int kThreads, uint32_t kUnits, bool kStream>
+hipError_t logprobs_blocks(TokenArgs a, uint32_t packs, hipStream_t st) {
+  a.parts = kThreads == 64 ? 1 : logit_parts(a.count, packs);  // (64: a.keys holds none)
+  a.part_packs = (packs + a.parts - 1) / a.parts;
+  a.parts = (packs + a.part_packs - 1) / a.part_packs;
+  const uint32_t blocks = (uint32_t)std::min((uint64_t)a.count * a.parts, kMostBlocks);
   if (a.top)
-    launch_k(tlc_token_logprobs_kernel<T, V, true>, (uint32_t)blocks, kLogThreads, st, a);
+    launch_k(tlc_token_logprobs_kernel<T, V, true, kThreads, kUnits, kStream>, blocks, kThreads,
+             st, a);
   else
-    launch_k(tlc_token_logprobs_kernel<T, V, false>, (uint32_t)blocks, kLogThreads, st, a);
-  hipError_t e = hipGetLastError();
-  if (e == hipSuccess && a.parts > 1) {
-    launch_k(tlc_token_join_kernel<T>, a.count, kLogThreads, st, a);
-    e = hipGetLastError();
-  }
-  return e;
+    launch_k(tlc_token_logprobs_kernel<T, V, false, kThreads, kUnits, kStream>, blocks, kThreads,
+             st, a);
+  return hipGetLastError();
 }
 
 template <class T>
-hipError_t logprobs_rows(TokenArgs a, hipStream_t st) {
+hipError_t logprobs_rows(const TokenArgs& a, hipStream_t st) {
   constexpr int V = 16 / sizeof(T);
-  const uint32_t packs = a.vocab < V ? a.vocab : (a.vocab + V - 1) / V;
-  a.parts = logit_parts(a.count, packs);
-  a.part_packs = (packs + a.parts - 1) / a.parts;
-  a.parts = (packs + a.part_packs - 1) / a.part_packs;
-  return a.vocab < V ? logprobs_packs<T, 1>(a, st) : logprobs_packs<T, V>(a, st);
+  const uint32_t packs = (a.vocab + V - 1) / V;
+  if (a.vocab < V) return logprobs_blocks<T, 1, 64, 1, false>(a, a.vocab, st);
+  if (wave_rows(a.count, packs, a.top))
+    return packs <= 2 * 64 ? logprobs_blocks<T, V, 64, 2, false>(a, packs, st)
+                           : logprobs_blocks<T, V, 64, 4, false>(a, packs, st);
+  if ((uint64_t)a.count * packs * 16 >= kStreamBytes)
+    return logprobs_blocks<T, V, kLogThreads, 8, true>(a, packs, st);
+  return packs <= 2 * kLogThreads ? logprobs_blocks<T, V, kLogThreads, 2, false>(a, packs, st)
+                                  : logprobs_blocks<T, V, kLogThreads, 4, false>(a, packs, st);
 }
 
 template <class In, class Out>

@@ -61,6 +61,7 @@ struct tlc_train {
   std::vector<Span> spans, spans_ok, adamw_ok;
   // token log probabilities: the parts of cut rows; AdamW: the blocks' tickets
   LogitPart* logit_part = nullptr;
+  uint32_t* logit_tickets = nullptr;
   uint64_t* logit_keys = nullptr;
   uint32_t* tickets = nullptr;
 };
@@ -259,15 +260,17 @@ TLC_API int tlc_train_create(tlc_train** out, size_t max_tokens, size_t max_rows
   }
   c->slot_pieces =
       max_tensors > std::min(kArgTensors, kAdamTensors) ? kNormBlocks + max_tensors : 0;
-  // layout: partial sums | tickets | logits' parts | their keys | a long list's pieces |
+  // layout: partial sums | tickets, zeroed | logits' parts | their keys | a long list's pieces |
   //         sorted tokens, twice | counts of the sort | touched rows | partial rows
   size_t off = round_up(kNormBlocks * sizeof(double), 256);
   const size_t off_tickets = off;
   off = round_up(off + kTicketBytes, 256);
+  const size_t off_logit_tickets = off;
+  off = round_up(off + kLogBlocks / 2 * kTicketWords * sizeof(uint32_t), 256);
   const size_t off_logit_part = off;
   off = round_up(off + kLogBlocks * sizeof(LogitPart), 256);
   const size_t off_logit_keys = off;
-  off = round_up(off + kLogBlocks * TLC_MAX_TOP * sizeof(uint64_t), 256);
+  off = round_up(off + kLogBlocks * kLogThreads * sizeof(uint64_t), 256);
   const size_t off_pieces = off;
   off = round_up(off + c->slot_pieces * sizeof(Piece), 256);
   size_t off_sort[4];
@@ -285,7 +288,7 @@ TLC_API int tlc_train_create(tlc_train** out, size_t max_tokens, size_t max_rows
                            sizeof(float), 256);
   e = hipMalloc(&c->ws, off);
   if (e == hipSuccess) e = hipMemset((uint8_t*)c->ws + off_touched, 0, max_rows);
-  if (e == hipSuccess) e = hipMemset((uint8_t*)c->ws + off_tickets, 0, kTicketBytes);
+  if (e == hipSuccess) e = hipMemset((uint8_t*)c->ws + off_tickets, 0, off_logit_part - off_tickets);
   if (e == hipSuccess) e = hipDeviceSynchronize();
   if (e == hipSuccess) e = hipHostMalloc((void**)&c->bad, 256, hipHostMallocDefault);
   if (e == hipSuccess) e = hipHostGetDevicePointer((void**)&c->bad_dev, c->bad, 0);
@@ -304,6 +307,7 @@ TLC_API int tlc_train_create(tlc_train** out, size_t max_tokens, size_t max_rows
   uint8_t* base = (uint8_t*)c->ws;
   c->partials = (double*)base;
   c->tickets = (uint32_t*)(base + off_tickets);
+  c->logit_tickets = (uint32_t*)(base + off_logit_tickets);
   c->logit_part = (LogitPart*)(base + off_logit_part);
   c->logit_keys = (uint64_t*)(base + off_logit_keys);
   c->pieces = (Piece*)(base + off_pieces);
@@ -524,6 +528,7 @@ TLC_API int tlc_token_logprobs(tlc_train* c, const void* logits, int type, size_
   a.top_ids = top_ids;
   a.part = c->logit_part;
   a.keys = c->logit_keys;
+  a.tickets = c->logit_tickets;
   return launched(c, launch_token_logprobs(a, type, c->stream), fn);
 }
 

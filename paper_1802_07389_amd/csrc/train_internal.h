@@ -211,6 +211,10 @@ __device__ __forceinline__ void put_result(tlc_norm_result* r, Clip c) {
   r->reserved = 0u;
 }
 
+// Words from one counter of blocks to the next: each has a cache line of its own,
+// where atomics come one after the other.
+constexpr uint32_t kTicketWords = 32;
+
 // ---- token log probabilities
 constexpr uint32_t kLogThreads = 256;
 // A row, or a part of one: its largest logit (at least -FLT_MAX) and sums by it.
@@ -232,18 +236,38 @@ struct TokenArgs : LogitArgs {
   uint32_t top;
   float* top_logprobs;
   int32_t* top_ids;
-  // rows cut into parts: the parts' sums and `top` keys each
+  // rows cut into parts: the parts' sums and a key for each of their threads
   uint32_t parts, part_packs;
   LogitPart* part;
   uint64_t* keys;
+  uint32_t* tickets;  // of a row's blocks that are done; zero between calls
 };
-// Parts of a row: where the rows alone leave CUs idle, as many as make
-// kLogBlocks blocks, each with a pack for every thread at least.
-constexpr uint32_t kLogBlocks = 1024, kLogMaxParts = kLogThreads;
+// Packs of 16 bytes a row.  Short rows take a wave each (8192 rows of 2048 fp32
+// values 12.7 us, in blocks 17; with five alternatives 17.7 | 48.6), longer ones where
+// there are many or no alternatives are asked for (packs up to kManyPacks: 4096 rows
+// of 8192 bf16 values with twenty 22.9 | 34.5, 64 such rows 11.1 | 7.5).  More than
+// kWaveTop alternatives are half of a wave's lanes, whose largest then say little.
+constexpr uint32_t kWavePacks = 512, kManyPacks = 1024, kManyRows = 2048, kWaveTop = 32;
+inline bool wave_rows(uint32_t count, uint32_t packs, uint32_t top) {
+  return top <= kWaveTop &&
+         (packs <= kWavePacks || (packs <= kManyPacks && (top == 0 || count >= kManyRows)));
+}
+// Parts of a row: where the rows alone leave CUs idle, as many as make kLogBlocks
+// blocks, of kPartPacks packs at least (1 row of 131072 fp32 values with twenty
+// alternatives 11.3 us; in parts of half | a quarter 12.4 | 16; 64 such rows 15.6, in 1024
+// blocks 19.9: the last block of a row reads a key for each thread of the others).
+constexpr uint32_t kLogBlocks = 512, kLogMaxParts = 256, kPartPacks = 4096;
 inline uint32_t logit_parts(uint32_t count, uint32_t packs) {
   const uint32_t want = std::min(kLogBlocks / count, kLogMaxParts);
-  return std::max(1u, std::min(want, packs / kLogThreads));
+  return std::max(1u, std::min(want, packs / kPartPacks));
 }
+// Groups of four threads' segments: up to so many alternatives.
+constexpr uint32_t kQuadTop = 32;
+// Logits of the last-level cache's size and more are read past it, eight packs of
+// a thread in flight (8192 rows of 65536 bf16 values, 966 MB: 143 us, 6.75 TB/s;
+// through the cache 158, with four packs 165, past it 148; 64 rows of 131072 fp32
+// values, which the cache holds, 18.7 | 19.8 past it).
+constexpr uint64_t kStreamBytes = 256u << 20;
 hipError_t launch_token_logprobs(const TokenArgs& a, int type, hipStream_t st);
 
 struct TokenGradArgs : LogitArgs {
@@ -327,9 +351,8 @@ struct AdamArgs {
   tlc_norm_result* result;  // NULL: no clipping
   uint32_t* tickets;        // the step's last launch: counts its blocks; else NULL
 };
-// The counters: of the groups, and of each group's blocks, each in a cache line
-// of its own; zero between calls.
-constexpr uint32_t kTicketGroups = 64, kTicketWords = 32;
+// The counters: of the groups, and of each group's blocks; zero between calls.
+constexpr uint32_t kTicketGroups = 64;
 constexpr size_t kTicketBytes = (1 + kTicketGroups) * kTicketWords * sizeof(uint32_t);
 static_assert(sizeof(AdamList) + sizeof(AdamArgs) <= 3840, "kernel arguments end at 4096 bytes");
 template <class List>
