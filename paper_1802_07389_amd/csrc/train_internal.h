@@ -266,7 +266,8 @@ constexpr uint32_t kQuadTop = 32;
 // Logits of the last-level cache's size and more are read past it, eight packs of
 // a thread in flight (8192 rows of 65536 bf16 values, 966 MB: 143 us, 6.75 TB/s;
 // through the cache 158, with four packs 165, past it 148; 64 rows of 131072 fp32
-// values, which the cache holds, 18.7 | 19.8 past it).
+// values, which the cache holds, 18.7 | 19.8 past it).  Gradients of that size are
+// read and written past it (8192 x 131072 bf16 values 662 | 677 us).
 constexpr uint64_t kStreamBytes = 256u << 20;
 hipError_t launch_token_logprobs(const TokenArgs& a, int type, hipStream_t st);
 
@@ -277,7 +278,10 @@ struct TokenGradArgs : LogitArgs {
   void* out;
   uint64_t out_stride;
   uint32_t slices;            // blocks of a row
+  uint32_t row0, rows;        // of short rows, a launch's
 };
+constexpr uint32_t kGradUnits = 2, kShortPacks = 256;
+
 hipError_t launch_token_grad(const TokenGradArgs& a, int type, int out_type, hipStream_t st);
 
 // ---- AdamW
