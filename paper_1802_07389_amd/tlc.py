@@ -703,6 +703,8 @@ class AdamWList:
         for p in self.params:
             if not p.is_contiguous():
                 raise ValueError("every tensor of a list must be contiguous")
+        self.device = self.params[0].device if self.params else torch.device(
+            "cuda", torch.cuda.current_device())
         self.count = len(self.params)
         self.ns = [p.numel() for p in self.params]
         codes = [_type_of(p, "param") for p in self.params]
@@ -719,8 +721,7 @@ class AdamWList:
         self.scales = list(states[2]) if bits == 8 else None
         self.clock = clock
         if clock is None:
-            device = self.params[0].device if self.params else "cuda"
-            self.clock = torch.tensor([0, 0x3f800000], device=device)  # 0 steps, 1.0f
+            self.clock = torch.tensor([0, 0x3f800000], device=self.device)  # 0 steps, 1.0f
         self.clock_ptr = _dev_of(self.clock, "clock", torch.int64, (2,))
         self.step, self.lr_scale = self.clock[0], self.clock.view(torch.float32)[2]
         self.deltas = None if deltas is None else list(deltas)
@@ -740,6 +741,12 @@ class AdamWList:
         self.grads = None if grads is None else list(grads)
         self.grad_args = None if grads is None else self.lay_out(self.grads)
         self.options, self.options_ptr, self.rates = None, None, None
+        self._check_device(self.params + self.exp_avgs + self.exp_avg_sqs + [self.clock]
+                           + (self.scales or []) + (self.deltas or []))
+
+    def _check_device(self, tensors):
+        if any(t.device != self.device for t in tensors):
+            raise ValueError("the tensors of a list are on one device")
 
     def _ptrs(self, tensors, dtype, name):
         if len(tensors) != self.count:
@@ -755,6 +762,7 @@ class AdamWList:
         grads = list(grads)
         if [g.numel() for g in grads] != self.ns:
             raise ValueError("params and grads differ in their sizes")
+        self._check_device(grads)
         for g in grads:
             if not g.is_contiguous():
                 raise ValueError("every tensor of a list must be contiguous")
@@ -785,6 +793,7 @@ class TrainContext:
         self.device = torch.device(device) if device is not None else torch.device(
             "cuda", torch.cuda.current_device())
         with torch.cuda.device(self.device):
+            self.index = torch.cuda.current_device()
             self.stream = stream if stream is not None else torch.cuda.current_stream()
             self.handle = tlc_train_create(int(max_tokens), int(max_rows), int(max_dim),
                                            int(max_tensors), self.stream.cuda_stream)
@@ -872,6 +881,11 @@ class TrainContext:
                                       out_ptrs))
         return r
 
+    def _check_device(self, *tensors):
+        for t in tensors:
+            if t is not None and t.get_device() != self.index:
+                raise ValueError(f"a tensor is not on the context's device, cuda:{self.index}")
+
     def token_result(self, shape, top=0):
         """A result buffer for rows of `shape` (a number or a shape) with `top`
         alternatives each, to pass to token_logprobs()."""
@@ -886,6 +900,7 @@ class TrainContext:
             out = self.token_result(shape, top)
         elif out.shape != shape or out.top != top:
             raise ValueError("out has the wrong size")
+        self._check_device(logits, targets, out.buffer)
         _check(lib.tlc_token_logprobs(
             self.handle, *rows, scale, *ids, ignore_id, out.buffer.data_ptr(), top,
             out.top_logprobs.data_ptr() if top else None, out.top_ids.data_ptr() if top else None))
@@ -907,6 +922,7 @@ class TrainContext:
         grads = [None if g is None else _dev_of(g, name, torch.float32, shape) for g, name in
                  ((grad_logprob, "grad_logprob"), (grad_entropy, "grad_entropy"))]
         out_ptr, out_code, out_stride = _matrix(out, "out")
+        self._check_device(logits, targets, buffer, grad_logprob, grad_entropy, out)
         _check(lib.tlc_token_logprobs_grad(
             self.handle, *rows, scale, *ids, ignore_id,
             _dev_of(buffer, "results", torch.float32, (*shape, 4)), *grads, out_ptr, out_code,
@@ -930,6 +946,8 @@ class TrainContext:
         that is not finite the step is left out."""
         if (max_norm is None) != (result is None):
             raise ValueError("max_norm and result belong together")
+        if weights.device.index != self.index:
+            raise ValueError(f"the weights are not on the context's device, cuda:{self.index}")
         grad_args = weights.grad_args if grads is None else weights.lay_out(grads)
         if grad_args is None:
             raise ValueError("no gradients are given, and the list has none")
