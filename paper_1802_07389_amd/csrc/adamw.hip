@@ -59,10 +59,10 @@ constexpr uint32_t steps_of(int bits) { return bits == 32 ? 4 : 2; }
 // Values k to k + 3 of x, those from n on 0.  No load waits for a condition: at
 // the end a pack is moved back to end with the values, and its own ones shifted
 // down; of fewer values than a pack, value by value.
-template <bool kFull, class T>
+template <bool kFull, bool kStream, class T>
 __device__ __forceinline__ Pack<T, V> load_some(const void* x, uint32_t k, uint32_t n) {
   const T* p = static_cast<const T*>(x);
-  if (kFull) return load_pack<T, V>(p + k);
+  if (kFull) return load_pack<T, V, kStream>(p + k);
   Pack<T, V> r;
   if (n < V) {
 #pragma unroll
@@ -88,11 +88,11 @@ __device__ __forceinline__ Pack<T, V> load_some(const void* x, uint32_t k, uint3
   }
   return r;
 }
-template <bool kFull, class T>
+template <bool kFull, bool kStream, class T>
 __device__ __forceinline__ void store_some(void* x, uint32_t k, uint32_t n, const Pack<T, V>& r) {
   T* p = static_cast<T*>(x);
   if (kFull || k + V <= n) {
-    store_pack<T, V>(p + k, r);
+    store_pack<T, V, kStream>(p + k, r);
     return;
   }
 #pragma unroll
@@ -153,17 +153,17 @@ struct Chunk {
   float sm[kSteps], sv[kSteps];
 };
 
-template <bool kFull, class P, class G, int kBits, uint32_t kSteps>
+template <bool kFull, bool kStream, class P, class G, int kBits, uint32_t kSteps>
 __device__ __forceinline__ void load_chunk(Chunk<P, G, kBits, kSteps>& c, const AdamPiece& t,
                                            uint32_t k0) {
   using S = std::conditional_t<kBits == 32, float, uint8_t>;
 #pragma unroll
   for (uint32_t u = 0; u < kSteps; ++u) {
     const uint32_t k = k0 + u * kStride + threadIdx.x * V;
-    c.p[u] = load_some<kFull, P>(t.p, k, t.n);
-    c.g[u] = load_some<kFull, G>(t.g, k, t.n);
-    c.m[u] = load_some<kFull, S>(t.m, k, t.n);
-    c.v[u] = load_some<kFull, S>(t.v, k, t.n);
+    c.p[u] = load_some<kFull, kStream, P>(t.p, k, t.n);
+    c.g[u] = load_some<kFull, kStream, G>(t.g, k, t.n);
+    c.m[u] = load_some<kFull, kStream, S>(t.m, k, t.n);
+    c.v[u] = load_some<kFull, kStream, S>(t.v, k, t.n);
     if constexpr (kBits == 8) {
       // (a wave beyond the end takes the last block's: its values are 0)
       const uint32_t b = umin32(k, t.n - 1) / TLC_STATE_BLOCK;
@@ -173,7 +173,7 @@ __device__ __forceinline__ void load_chunk(Chunk<P, G, kBits, kSteps>& c, const 
   }
 }
 
-template <bool kFull, class P, class G, int kBits, uint32_t kSteps>
+template <bool kFull, bool kStream, class P, class G, int kBits, uint32_t kSteps>
 __device__ __forceinline__ void step_chunk(const Chunk<P, G, kBits, kSteps>& c,
                                            const AdamPiece& t, uint32_t k0, const AdamArgs& a,
                                            const Factors& f) {
@@ -210,8 +210,8 @@ __device__ __forceinline__ void step_chunk(const Chunk<P, G, kBits, kSteps>& c,
       q.set(e, adam_step(old, f.coef * c.g[u].get(e), m[e], v[e], a, f));
       d.set(e, q.get(e) - old);
     }
-    store_some<kFull, P>(t.p, k, t.n, q);
-    if (t.delta) store_some<kFull, float>(t.delta, k, t.n, d);
+    store_some<kFull, kStream, P>(t.p, k, t.n, q);
+    if (t.delta) store_some<kFull, kStream, float>(t.delta, k, t.n, d);
     Pack<S, V> pm, pv;
     if constexpr (kBits == 32) {
 #pragma unroll
@@ -263,8 +263,8 @@ __device__ __forceinline__ void step_chunk(const Chunk<P, G, kBits, kSteps>& c,
         t.scales[k / TLC_STATE_BLOCK * 2 + 1] = sv;
       }
     }
-    store_some<kFull, S>(t.m, k, t.n, pm);
-    store_some<kFull, S>(t.v, k, t.n, pv);
+    store_some<kFull, kStream, S>(t.m, k, t.n, pm);
+    store_some<kFull, kStream, S>(t.v, k, t.n, pv);
   }
 }
 
@@ -296,6 +296,21 @@ __device__ __forceinline__ bool last_to_read(uint32_t* tickets, int64_t step) {
   return true;
 }
 
+constexpr uint32_t kLine = 128, kLongPiece = 16 * kStride;
+
+// A piece of n values of fp32 states without its first `head`.
+__device__ __forceinline__ AdamPiece adam_rest(AdamPiece t, uint32_t head, uint32_t n, uint32_t p,
+                                               uint32_t g) {
+  t.p = static_cast<uint8_t*>(t.p) + head * p;
+  t.g = static_cast<const uint8_t*>(t.g) + head * g;
+  t.m = static_cast<float*>(t.m) + head;
+  t.v = static_cast<float*>(t.v) + head;
+  t.delta = t.delta ? t.delta + head : nullptr;
+  t.n = n - head;
+  t.k0 += head;
+  return t;
+}
+
 template <int kBits>
 struct Step {
   const AdamArgs& a;
@@ -311,26 +326,47 @@ struct Step {
     ready = true;
   }
 
-  template <class P, class G, uint32_t kSteps, bool kFull>
+  template <class P, class G, uint32_t kSteps, bool kFull, bool kStream = false>
   __device__ __forceinline__ void chunk(const AdamPiece& t, uint32_t k) {
     Chunk<P, G, kBits, kSteps> c;
-    load_chunk<kFull>(c, t, k);
+    load_chunk<kFull, kStream>(c, t, k);
     wait();
     if (f.skip) {
       // a change of nothing, so that the codec is not given the last step's
       if (t.delta)
 #pragma unroll
         for (uint32_t u = 0; u < kSteps; ++u)
-          store_some<kFull, float>(t.delta, k + u * kStride + threadIdx.x * V, t.n, {});
+          store_some<kFull, kStream, float>(t.delta, k + u * kStride + threadIdx.x * V, t.n, {});
       return;
     }
-    step_chunk<kFull>(c, t, k, a, f);
+    step_chunk<kFull, kStream>(c, t, k, a, f);
   }
 
   template <class P, class G>
-  __device__ __forceinline__ void piece(const AdamPiece& t) {
+  __device__ __forceinline__ void piece(AdamPiece t) {
     constexpr uint32_t kSteps = steps_of(kBits);
     uint32_t k = 0;
+    if constexpr (kBits == 32) {
+      // Long pieces (which a list has only where it is larger than the last-level
+      // cache) go on from where a line of p begins: the states of a flat buffer's
+      // tensors begin lines there too.  Whole lines are written, and where all of
+      // them do, past the cache (148 tensors of 100M values at odd offsets 571 us
+      // without, 549 with whole lines, 525 past the cache; partial lines past the cache
+      // 640).  8-bit blocks stay where they are.
+      if (t.n >= kLongPiece) {
+        const uint32_t head = (uint32_t)(-reinterpret_cast<uintptr_t>(t.p) % kLine) / sizeof(P);
+        if (head) {
+          const uint32_t n = t.n;
+          t.n = head;
+          chunk<P, G, 1, false>(t, 0);
+          t = adam_rest(t, head, n, sizeof(P), sizeof(G));
+        }
+        if ((reinterpret_cast<uintptr_t>(t.p) | reinterpret_cast<uintptr_t>(t.m) |
+             reinterpret_cast<uintptr_t>(t.v) | reinterpret_cast<uintptr_t>(t.delta)) % kLine == 0)
+          for (; t.n - k >= kSteps * kStride; k += kSteps * kStride)
+            chunk<P, G, kSteps, true, true>(t, k);
+      }
+    }
     for (; t.n - k >= kSteps * kStride; k += kSteps * kStride) chunk<P, G, kSteps, true>(t, k);
     for (; t.n - k >= kStride; k += kStride) chunk<P, G, 1, true>(t, k);
     if (k < t.n) chunk<P, G, 1, false>(t, k);

@@ -330,6 +330,23 @@ def test_captured_and_replayed(bits):
         c.sync()
 
 
+@pytest.mark.parametrize("kinds", [("f32", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("offset,state_offset", [(0, 0), (3, 3), (3, 1), (31, 31)])
+def test_long_pieces(ctx, kinds, offset, state_offset):
+    """Lists beyond the last-level cache, whose weights begin within a line, with
+    their states alike or not."""
+    sizes = [17_000_003, 5, 17_500_001]
+    w = make(ctx, 14, sizes, kinds, 32, offset)
+    if state_offset != offset:
+        states = [[at_offset(torch.zeros(n, device="cuda"), state_offset) for n in sizes]
+                  for _ in range(2)]
+        w = ctx.adamw_list(w.params, w.grads, 32, w.deltas, states)
+    want = expected(w, w.grads, 1)
+    ctx.adamw(w, **RATES)
+    ctx.sync()
+    check(w, want)
+
+
 def test_values_beyond_31_bits(ctx):
     """A tensor whose last values lie past 2^31, and their codes' dither."""
     n = (1 << 31) + 300
