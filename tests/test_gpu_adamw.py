@@ -281,6 +281,37 @@ def test_changes_in_the_gradients_place(ctx, bits):
     assert all(torch.equal(x, y) for x, y in zip(a.params, b.params))
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_many_calls_in_a_row(ctx, bits):
+    """Long lists of the norm and of steps, none waited for: more of them than
+    the context has places in host memory to lay a list out."""
+    sizes = [(53 * i) % 900 + 1 for i in range(150)]
+    w = make(ctx, 15, sizes, ("f32",), bits)
+    other = make(ctx, 16, sizes[::-1], ("bf16", "f32"), bits)
+    norm = math.sqrt(sum(float(g.double().square().sum()) for g in w.grads))
+    state = [ref.numpy_of(p) for p in w.params]
+    m = [np.zeros_like(p) for p in state]
+    v = [np.zeros_like(p) for p in state]
+    grads = [ref.numpy_of(g) for g in w.grads]
+    results = []
+    for t in range(1, 14):
+        results.append(ctx.grad_norm(w.grads))
+        ctx.adamw(w, **RATES)
+        ctx.adamw(other, **RATES)
+    ctx.sync()
+    assert all(abs(float(r.norm) - norm) <= 2 * U * norm for r in results)
+    for t in range(1, 14):
+        f = ref.factors(t, **RATES)
+        for i, g in enumerate(grads):
+            state[i], m[i], v[i] = ref.fp32_step(state[i], g, m[i], v[i], 1.0, f)
+            if bits == 8:
+                q, c, s = ref.encode(m[i], v[i], t)
+                m[i] = ref.decode(torch.from_numpy(q), torch.float8_e4m3fn, s, 0)
+                v[i] = ref.decode(torch.from_numpy(c), torch.float8_e5m2, s, 1)
+    assert all(same_bits(p, torch.from_numpy(x)) for p, x in zip(w.params, state))
+    assert int(w.step) == int(other.step) == 13
+
+
 def test_gradients_of_the_call(ctx):
     w = make(ctx, 11, [300, 40], ("f32",), 32)
     fresh = [torch.randn(300, device="cuda").bfloat16(), torch.randn(40, device="cuda")]

@@ -177,6 +177,48 @@ def test_nan_and_infinity_stay_in_their_rows(ctx, kind, bad, count):
     assert bool(g[keep].isfinite().all())
 
 
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("count,vocab", [(5, 100_003), (3, 1_000_003), (1, 1 << 24), (200, 65_536)])
+def test_rows_in_parts(ctx, kind, count, vocab):
+    """Rows that several blocks share (up to 256), some of them left out, empty or
+    of NaN, and alternatives that lie in one part, in all, or are all equal."""
+    x = rows_of(count, count, vocab, kind, 3)
+    t = targets_of(vocab, count, vocab, torch.int32, 0.3)
+    for top in (0, 1, 20, 64):
+        check(ctx, x, t, 0.9, top)
+    x[0, 40:60] = 30.0                       # the largest in one part, equal
+    x[-1] = -2.0                             # all equal
+    t[-1] = vocab - 1
+    check(ctx, x, t, 1.0, 33)
+    x[-1].copy_(torch.arange(vocab, device="cuda") * (8.0 / vocab))
+    check(ctx, x, t, 1.0, 64)
+    if count > 2:
+        x[1], x[2, vocab - 2] = -math.inf, math.nan
+        t[1], t[2] = 3, 4
+        r = ctx.token_logprobs(x, t, top=20)
+        ctx.sync()
+        assert bool(r.buffer[2].isnan().all()) and bool((r.top_ids[2] == -1).all())
+        assert bool((r.top_logprobs[1] == -math.inf).all()) and float(r.entropy[1]) == 0.0
+        assert r.top_ids[1].tolist() == list(range(20))
+        assert bool(r.buffer[0].isfinite().all())
+
+
+def test_more_rows_than_blocks(ctx):
+    """Millions of short rows: a block takes several."""
+    count, vocab = 4_300_000, 9
+    x = rows_of(70, count, vocab, "bf16")
+    t = targets_of(71, count, vocab, ignored=0.1)
+    r = check(ctx, x, t, 1.0, 2)
+    g = ctx.token_logprobs_grad(x, t, r, torch.ones(count, device="cuda"))
+    ctx.sync()
+    for rows in (slice(0, 1000), slice(count - 1000, count)):
+        part = ctx.token_logprobs_grad(x[rows].contiguous(), t[rows].contiguous(),
+                                       r.buffer[rows].contiguous(),
+                                       torch.ones(1000, device="cuda"))
+        ctx.sync()
+        assert torch.equal(g[rows], part)
+
+
 def test_rows_left_out_are_not_read_into_anything(ctx):
     x = rows_of(8, 50, 999, "f32")
     t = targets_of(9, 50, 999, ignored=0.5)
