@@ -54,10 +54,7 @@ __device__ __forceinline__ float adam_step(float p, float g, float& m, float& v,
 
 constexpr int V = 4;  // neighbouring values of a thread
 constexpr uint32_t kStride = kAdamThreads * V;
-// Of them, in flight: a wave's are whole blocks of 8-bit states (100M values, two |
-// four: 590 | 569 us of 32 bits, 330 | 332 of 8, one 363; few values, which have no
-// wave to spare, in short pieces one at a time).
-constexpr uint32_t steps_of(int bits) { return bits == 32 ? 4 : 2; }
+static_assert(kStride == kAdamUnit, "a unit is a pack of every thread");
 
 // Values k to k + 3 of x, those from n on 0.  No load waits for a condition: at
 // the end a pack is moved back to end with the values, and its own ones shifted
@@ -302,7 +299,7 @@ __device__ __forceinline__ bool last_to_read(uint32_t* tickets, int64_t step) {
   return true;
 }
 
-constexpr uint32_t kLine = 128, kLongPiece = 16 * kStride;
+constexpr uint32_t kLine = 128;
 
 // A piece of n values of fp32 states without its first `head`.
 __device__ __forceinline__ AdamPiece adam_rest(AdamPiece t, uint32_t head, uint32_t n, uint32_t p,
@@ -350,16 +347,16 @@ struct Step {
 
   template <class P, class G>
   __device__ __forceinline__ void piece(AdamPiece t) {
-    constexpr uint32_t kSteps = steps_of(kBits);
+    constexpr uint32_t kSteps = adam_steps(kBits);
     uint32_t k = 0;
     if constexpr (kBits == 32) {
-      // Long pieces (which a list has only where it is larger than the last-level
-      // cache) go on from where a line of p begins: the states of a flat buffer's
-      // tensors begin lines there too.  Whole lines are written, and where all of
-      // them do, past the cache (148 tensors of 100M values at odd offsets 571 us
-      // without, 549 with whole lines, 525 past the cache; partial lines past the cache
-      // 640).  8-bit blocks stay where they are.
-      if (t.n >= kLongPiece) {
+      // Pieces of a list larger than the last-level cache go on from where a line of p
+      // begins: the states of a flat buffer's tensors begin lines there too.  Whole
+      // lines are written, and where all of them do, past the cache (148 tensors of
+      // 100M values at odd offsets, 2048 pieces: 571 us without, 549 with whole lines,
+      // 525 past the cache; partial lines past the cache 640).  8-bit blocks stay where
+      // they are.
+      if (a.stream && t.n >= kSteps * kStride) {  // (more values than a head has)
         const uint32_t head = (uint32_t)(-reinterpret_cast<uintptr_t>(t.p) % kLine) / sizeof(P);
         if (head) {
           const uint32_t n = t.n;
@@ -419,7 +416,7 @@ __global__ __launch_bounds__(kAdamThreads) void tlc_adamw_kernel(List list, Adam
 
 template <class List>
 hipError_t launch_adamw(const List& list, const AdamArgs& a, int state_type, hipStream_t st) {
-  const uint32_t grid = std::max(1u, std::min(list.n, kNormBlocks));
+  const uint32_t grid = std::max(1u, std::min(list.n, kAdamPieces));
   if (state_type == TLC_STATE_8BIT)
     launch_k(tlc_adamw_kernel<List, 8>, grid, kAdamThreads, st, list, a);
   else

@@ -20,7 +20,8 @@ namespace {
 // pieces).
 constexpr int kGroups = 2, kGroupSlots = 4;
 constexpr size_t kSlotPiece = sizeof(AdamPiece);  // bytes of the largest piece
-static_assert(sizeof(Piece) <= kSlotPiece, "slots hold pieces of either kind");
+static_assert(sizeof(Piece) <= kSlotPiece && kNormBlocks <= kAdamPinned,
+              "slots hold pieces of either kind");
 constexpr size_t kMaxListValues = (size_t)1 << 40;
 constexpr float kMaxLogitScale = 1e18f;
 
@@ -259,7 +260,7 @@ TLC_API int tlc_train_create(tlc_train** out, size_t max_tokens, size_t max_rows
     return hip_fail(e, "hipGetDevice");
   }
   c->slot_pieces =
-      max_tensors > std::min(kArgTensors, kAdamTensors) ? kNormBlocks + max_tensors : 0;
+      max_tensors > std::min(kArgTensors, kAdamTensors) ? kAdamPinned + max_tensors : 0;
   // layout: partial sums | tickets, zeroed | logits' parts | their keys | a long list's pieces |
   //         sorted tokens, twice | counts of the sort | touched rows | partial rows
   size_t off = round_up(kNormBlocks * sizeof(double), 256);
@@ -747,7 +748,7 @@ AdamList adam_list(const AdamCall& l, size_t first, size_t* next) {
   for (; i < l.count && count < kAdamTensors; ++i)
     if (l.ns[i]) total += l.ns[i], ++count;
   *next = i;
-  r.len = adam_piece_values(total, count, kAdamUnit);
+  r.len = adam_piece_values(total, count, kAdamUnit, kAdamPieces);
   r.state_bytes = l.small() ? 1 : 4;
   for (i = first; i < *next; ++i) {
     if (l.ns[i] == 0) continue;
@@ -760,7 +761,8 @@ AdamList adam_list(const AdamCall& l, size_t first, size_t* next) {
 
 AdamPinned adam_pinned(const AdamCall& l, size_t total, AdamPiece* host, const AdamPiece* dev) {
   AdamPinned r = {dev, 0};
-  const size_t len = adam_piece_values(total, l.count, 2 * kAdamUnit);
+  const size_t len = std::max(adam_piece_values(total, l.count, 2 * kAdamUnit, kAdamPinned),
+                              adam_steps(l.small() ? 8 : 32) * kAdamUnit);
   for (size_t i = 0; i < l.count; ++i) {
     const AdamTensor e = adam_tensor(l, i);
     const uint32_t types = (uint32_t)l.types[i] | (uint32_t)l.grad_types[i] << 2;
@@ -813,6 +815,7 @@ TLC_API int tlc_adamw(tlc_train* c, size_t count, void* const* params, const int
   a.max_norm = options->max_norm;
   a.clock = clock;
   a.result = result;
+  a.stream = l.total * 12 >= kStreamBytes;  // fp32 weights and states
   bool pinned = false;
   st = pins(c, count, &pinned);
   if (st) return st;

@@ -287,14 +287,21 @@ hipError_t launch_token_grad(const TokenGradArgs& a, int type, int out_type, hip
 // ---- AdamW
 constexpr uint32_t kAdamThreads = 256;
 constexpr uint32_t kAdamTensors = 64;  // of a launch
-// Pieces, about kNormBlocks of them at most as in a list of the norm, are multiples
-// of kAdamUnit values, four a thread, so that few values still fill the chip
-// (1000003 of 8 bits 8.0 us, in pieces of 4096 9.8); in pinned memory of twice as
-// many, as a piece takes 3 ns of the bus (335 tensors of 1.7M values 16.4 | 18.8 us
-// with 2048 | 1024).
-constexpr uint32_t kAdamUnit = 1024;
-inline uint32_t adam_piece_values(size_t total, size_t count, uint32_t unit) {
-  const size_t most = kNormBlocks - std::min<size_t>(count, kNormBlocks / 2);
+// Packs of four values a thread has in flight: a wave's are whole blocks of 8-bit
+// states (100M values, two | four: 590 | 569 us of 32 bits, 330 | 332 of 8, one
+// 363; few values, which have no wave to spare, in short pieces one at a time).
+constexpr uint32_t kAdamUnit = kAdamThreads * 4;
+constexpr uint32_t adam_steps(int bits) { return bits == 32 ? 4 : 2; }
+// A block takes a piece, or of very many several.  Pieces are multiples of
+// kAdamUnit values, so that few values still fill the chip (1000003 of 8 bits 7.5 us,
+// in pieces of 4096 9.8); in pinned memory no shorter than what a block has in flight,
+// as a piece takes 3 ns of the bus (335 tensors of 1.7M values, pieces of 1024 | 2048 | 4096: 18.8 | 16.4
+// | 14.4 us of 32 bits, 18.3 | 16.4 | 17.2 of 8).  Large lists make kAdamPieces of
+// them or fewer, pinned ones kAdamPinned (one tensor of 100M, 2048 | 4096 | 8192 | 16384
+// pieces: 505 | 493 | 485 | 488 us; 148 tensors 523 | 503 | 512 | 508).
+constexpr uint32_t kAdamPieces = 8192, kAdamPinned = 4096;
+inline uint32_t adam_piece_values(size_t total, size_t count, size_t unit, size_t pieces) {
+  const size_t most = pieces - std::min<size_t>(count, pieces / 2);
   const size_t units = (total + most * unit - 1) / (most * unit);
   return (uint32_t)(std::max<size_t>(units, 1) * unit);
 }
@@ -353,6 +360,7 @@ struct AdamArgs {
   float eps, max_norm;
   tlc_adamw_clock* clock;
   tlc_norm_result* result;  // NULL: no clipping
+  bool stream;              // the list is larger than the last-level cache
   uint32_t* tickets;        // the step's last launch: counts its blocks; else NULL
 };
 // The counters: of the groups, and of each group's blocks; zero between calls.
