@@ -5,10 +5,10 @@
 // with c = 1 - beta, a = lr / (1 - beta1^t), r = 1 / sqrt(1 - beta2^t), w = lr decay.
 // States of 8 bits hold 256 values by one scale, m as OCP E4M3 and v as OCP E5M2.
 // What bounds it: every tensor read and written once (28 bytes an fp32 value of
-// fp32 states, 16 of 8 bits): 100M fp32 weights with bf16 gradients 525 us (5.0 TB/s),
-// of 8-bit states, whose blocks begin within lines, 332 (4.2 TB/s; at even offsets
-// 307).  With raw square roots and quotients the latter took as long.  335 tensors of
-// 1.7M values 16 us, of which one launch and the read of the pieces over the bus are 8.
+// fp32 states, 16 of 8 bits): 148 tensors of 100M fp32 weights with bf16 gradients
+// 503 us (5.2 TB/s), of 8-bit states, whose blocks begin within lines, 312 (4.5 TB/s); one
+// tensor 484 and 290.  Raw square roots and quotients changed neither.  335 tensors of
+// 1.7M values 14 us, of which one launch and the read of the pieces over the bus are 8.
 #include <math.h>
 
 #include <type_traits>
