@@ -108,7 +108,7 @@ def check(ctx, x, targets, scale=1.0, top=0, out=None):
 
 SIZES = [(1, 1), (1, 2), (3, 3), (2, 7), (5, 8), (4, 9), (7, 63), (3, 64), (2, 255), (9, 257),
          (2, 1023), (3, 2047), (2, 2049), (1, 8191), (2, 8200), (3, 30011), (1, 131072),
-         (700, 1000), (1100, 515), (64, 20001), (1025, 4099)]
+         (700, 1000), (1100, 515), (64, 20001), (1025, 4099), (2100, 4001)]
 
 
 @pytest.mark.parametrize("count,vocab", SIZES)
