@@ -24,6 +24,9 @@ constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 // Exponents are clamped here where they multiply a probability of 0: a logit of
 // -inf adds 0 * kFar and not 0 * -inf.
 constexpr float kFar = -1e30f;
+// ln p that the gradient multiplies by p: below it p is 0 (2^-149 is exp(-103.3)),
+// and factors of up to 2^120 times it stay finite.
+constexpr float kGone = -128.0f;
 constexpr float kFarRef = 65536.0f;  // m c below it, which fp32 rounds by 2^-8 at most
 
 // A row's target: its column, kNoTarget where the call has none, kLeftOut where
@@ -509,7 +512,7 @@ __device__ __forceinline__ float grad_of(const GradRow& r, float scale, float x,
   const float z = x - r.max;
   const float p = exp2_of(z * (scale * kLog2e) - r.log_sum * kLog2e);
   float bonus = 0.0f;
-  if (kEntropy) bonus = r.fb * (fmaxf(z * scale - r.log_sum, kFar) + r.entropy);
+  if (kEntropy) bonus = r.fb * (fmaxf(z * scale - r.log_sum, kGone) + r.entropy);
   if (is_target)  // a (1 - p), without the loss of 1 - p near 1
     return r.fa * expm1f(z * scale - r.log_sum) + bonus * p;
   return (r.fa + bonus) * p;
