@@ -25,7 +25,7 @@ constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 // -inf adds 0 * kFar and not 0 * -inf.
 constexpr float kFar = -1e30f;
 // ln p that the gradient multiplies by p: below it p is 0 (2^-149 is exp(-103.3)),
-// and factors of up to 2^120 times it stay finite.
+// and the factors, below 2^109, times it stay finite.
 constexpr float kGone = -128.0f;
 constexpr float kFarRef = 65536.0f;  // m c below it, which fp32 rounds by 2^-8 at most
 
@@ -487,6 +487,7 @@ namespace {
 struct GradRow {
   int64_t target;
   float fa, fb;  // -scale times the gradients of the log probability and the entropy
+  float unit;    // of fa and fb
   float max, log_sum, entropy;
   bool live;     // else zeroes, taken at x = 0: the row is not read
 };
@@ -498,9 +499,14 @@ __device__ __forceinline__ GradRow grad_row(const TokenGradArgs& a, uint32_t row
   const float ga = a.grad_logprob ? a.grad_logprob[row] : 0.0f;
   const float gb = kEntropy ? a.grad_entropy[row] : 0.0f;
   r.live = r.target != kLeftOut && res.max != -INFINITY;
-  if (!r.live) return GradRow{-1, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, false};  // 0 at x = 0
-  r.fa = -(ga * a.scale);
-  r.fb = -(gb * a.scale);
+  if (!r.live) return GradRow{-1, 0.0f, 0.0f, 1.0f, 0.0f, 0.0f, 0.0f, false};  // 0 at x = 0
+  // factors near fp32's end and beyond it are held as multiples of 2^80, as what p
+  // leaves of them may be small
+  const bool large = fmaxf(fabsf(ga), fabsf(gb)) * a.scale > 0x1p100f;
+  const float s = large ? a.scale * 0x1p-80f : a.scale;
+  r.unit = large ? 0x1p80f : 1.0f;
+  r.fa = -(ga * s);
+  r.fb = -(gb * s);
   r.max = res.max;
   r.log_sum = res.log_sum;
   r.entropy = res.entropy;
@@ -514,8 +520,8 @@ __device__ __forceinline__ float grad_of(const GradRow& r, float scale, float x,
   float bonus = 0.0f;
   if (kEntropy) bonus = r.fb * (fmaxf(z * scale - r.log_sum, kGone) + r.entropy);
   if (is_target)  // a (1 - p), without the loss of 1 - p near 1
-    return r.fa * expm1f(z * scale - r.log_sum) + bonus * p;
-  return (r.fa + bonus) * p;
+    return (r.fa * expm1f(z * scale - r.log_sum) + bonus * p) * r.unit;
+  return (r.fa + bonus) * p * r.unit;
 }
 
 template <class In, class Out, int V, bool kEntropy>

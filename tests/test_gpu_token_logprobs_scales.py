@@ -96,3 +96,21 @@ def test_scales_and_masked_entries(ctx, kind, scale, count, vocab):
             for out in ("f32", "bf16"):
                 got = check_grad(ctx, x, t, r, a, bonus, scale, out)
                 assert bool(got.isfinite().all()) and bool((got[0] == 0).all())
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("scale,size", [(1e18, 1e21), (1e18, 1e25), (1e10, 1e30), (1.0, 1e37)])
+@pytest.mark.parametrize("count,vocab", [(40, 3000), (300, 40)])
+def test_factors_whose_product_with_the_scale_is_beyond_fp32(ctx, kind, scale, size, count, vocab):
+    """scale a and scale b may be: what they are multiplied by may be small, or 0."""
+    g = torch.Generator(device="cuda").manual_seed(count)
+    a, b = (torch.randn(count, device="cuda", generator=g) * size for _ in range(2))
+    t = targets_of(vocab, count, vocab, ignored=0.2)
+    x = rows_of(8, count, vocab, kind, 0, 1.0)
+    spread(x, scale, 6.0)
+    mask(x)
+    r = check(ctx, x, t, scale)
+    for one, bonus in ((a, None), (torch.zeros_like(a), b), (a, b), (a / size, b), (a, b / size)):
+        for out in ("f32", "bf16"):
+            got = check_grad(ctx, x, t, r, one, bonus, scale, out)
+            assert not bool(got.isnan().any())
