@@ -46,8 +46,13 @@ __device__ __forceinline__ int64_t target_of(const LogitArgs& a, uint32_t row, b
 // above it, so that differences of -inf do not arise): s0 = sum e, s1 = sum e t with
 // t = (x - m) c, e = 2^t, c = s log2(e).  NaN and +inf make s0 NaN.
 __device__ __forceinline__ float exp2_of(float t) { return __builtin_amdgcn_exp2f(t); }
+// f (x - m), rounded as the two steps: the difference is formed of halves, as it may be
+// beyond fp32 where the product is not.
+__device__ __forceinline__ float scaled_difference(float x, float m, float f) {
+  return __builtin_fmaf(x, 0.5f, m * -0.5f) * (f * 2.0f);
+}
 __device__ __forceinline__ LogitPart rebased(LogitPart p, float m, float c) {
-  const float d = fmaxf((p.m - m) * c, kFar), f = exp2_of(d);
+  const float d = fmaxf(scaled_difference(p.m, m, c), kFar), f = exp2_of(d);
   return LogitPart{m, f * p.s0, f * (p.s1 + d * p.s0)};
 }
 __device__ __forceinline__ LogitPart merged(LogitPart a, LogitPart b, float c) {
@@ -171,7 +176,7 @@ __device__ __forceinline__ tlc_token_result result_of(LogitPart p, float scale, 
     r.max = p.m;
     r.log_sum = logf(p.s0);
     r.entropy = fmaxf(r.log_sum - kLn2 * (p.s1 / p.s0), 0.0f);
-    r.logprob = has_target ? (x - p.m) * scale - r.log_sum : 0.0f;
+    r.logprob = has_target ? scaled_difference(x, p.m, scale) - r.log_sum : 0.0f;
   }
   return r;
 }
@@ -199,7 +204,8 @@ __device__ __forceinline__ void put_row(const TokenArgs& a, uint32_t row, LogitP
   }
   const uint64_t key = best[threadIdx.x];
   a.top_logprobs[at] =
-      r.max == -INFINITY ? -INFINITY : (key_logit(key) - r.max) * a.scale - r.log_sum;
+      r.max == -INFINITY ? -INFINITY
+                         : scaled_difference(key_logit(key), r.max, a.scale) - r.log_sum;
   a.top_ids[at] = (int32_t)~(uint32_t)key;
 }
 
@@ -262,7 +268,7 @@ __device__ __forceinline__ void add_packs(Lane& l, const Pack<T, V> (&r)[kUnits]
     for (uint32_t u = 0; u < kUnits; ++u)
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        const float t = own(e) ? (r[u].get(e) - m) * c : kFar, w = exp2_of(t);
+        const float t = own(e) ? scaled_difference(r[u].get(e), m, c) : kFar, w = exp2_of(t);
         s0 += w;
         s1 = __builtin_fmaf(w, fmaxf(t, kFar), s1);
       }
@@ -515,12 +521,12 @@ __device__ __forceinline__ GradRow grad_row(const TokenGradArgs& a, uint32_t row
 
 template <bool kEntropy>
 __device__ __forceinline__ float grad_of(const GradRow& r, float scale, float x, bool is_target) {
-  const float z = x - r.max;
-  const float p = exp2_of(z * (scale * kLog2e) - r.log_sum * kLog2e);
+  const float p = exp2_of(scaled_difference(x, r.max, scale * kLog2e) - r.log_sum * kLog2e);
+  const float z = scaled_difference(x, r.max, scale);
   float bonus = 0.0f;
-  if (kEntropy) bonus = r.fb * (fmaxf(z * scale - r.log_sum, kGone) + r.entropy);
+  if (kEntropy) bonus = r.fb * (fmaxf(z - r.log_sum, kGone) + r.entropy);
   if (is_target)  // a (1 - p), without the loss of 1 - p near 1
-    return (r.fa * expm1f(z * scale - r.log_sum) + bonus * p) * r.unit;
+    return (r.fa * expm1f(z - r.log_sum) + bonus * p) * r.unit;
   return (r.fa + bonus) * p * r.unit;
 }
 

@@ -114,3 +114,25 @@ def test_factors_whose_product_with_the_scale_is_beyond_fp32(ctx, kind, scale, s
         for out in ("f32", "bf16"):
             got = check_grad(ctx, x, t, r, one, bonus, scale, out)
             assert not bool(got.isnan().any())
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("scale,factor", [(0.5, 1.0), (3e-38, 1e20)])
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("count,vocab", SHAPES)
+def test_logits_further_apart_than_fp32_reaches(ctx, kind, scale, factor, masked, count, vocab):
+    """Differences of logits may be beyond fp32 where their products with the scale
+    are not."""
+    x = rows_of(9, count, vocab, kind, 0, 1.0)
+    x.copy_((x.double() * 1e38).clamp(-3e38, 3e38).to(x.dtype))
+    x[:, :2] = torch.tensor([3e38, -3e38], device="cuda")
+    if masked:
+        x[:, vocab // 2::3] = -math.inf
+    t = targets_of(vocab, count, vocab)
+    t[::3] = 1
+    r = check(ctx, x, t, scale)
+    assert bool(r.logprob[::3].isfinite().all())
+    g = torch.Generator(device="cuda").manual_seed(count)
+    a, b = (torch.randn(count, device="cuda", generator=g) * factor for _ in range(2))
+    for bonus in (None, b):
+        check_grad(ctx, x, t, r, a, bonus, scale, "f32")
