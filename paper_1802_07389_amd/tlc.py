@@ -948,6 +948,7 @@ class TrainContext:
             raise ValueError("max_norm and result belong together")
         if weights.device.index != self.index:
             raise ValueError(f"the weights are not on the context's device, cuda:{self.index}")
+        self._check_device(None if result is None else result.buffer)
         grad_args = weights.grad_args if grads is None else weights.lay_out(grads)
         if grad_args is None:
             raise ValueError("no gradients are given, and the list has none")
