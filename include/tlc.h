@@ -418,11 +418,15 @@ typedef struct tlc_token_result {
  *                 for none) hold the largest logits' log probabilities and
  *                 columns, the largest first, the lowest column first among
  *                 equal logits.
- * Sums are in fp32 in an order that the sizes alone fix.  Entries of -inf have
- * probability 0.  A row with no other entry has max, log_sum and log probabilities -inf
- * and entropy 0; its top_ids are its first columns.  A row that holds NaN or
- * +inf has NaN in its place, and top_ids -1.  No output may overlap another
- * argument. */
+ * Sums are in fp32 in an order that the sizes alone fix.  log_sum is the logarithm
+ * of a sum that holds the largest logit's own 1, which each addition may round by
+ * 2^-24: where a token is nearly certain, the error of log_sum, logprob and the
+ * target's gradient is absolute (a logit 20 above 99 others: 1 - p of 2.0e-7 may come
+ * out as 2.4e-7, one below 2^-24 as 0).
+ * Entries of -inf have probability 0.  A row with no other entry has max, log_sum and
+ * log probabilities -inf and entropy 0; its top_ids are its first columns.  A row that
+ * holds NaN or +inf has NaN in its place, and top_ids -1.  No output may overlap
+ * another argument. */
 int tlc_token_logprobs(tlc_train* ctx, const void* logits, int type, size_t count, size_t vocab,
                        size_t stride, float scale, const void* targets, int ids_type,
                        int64_t ignore_id, tlc_token_result* results, size_t top,

@@ -525,7 +525,9 @@ __device__ __forceinline__ float grad_of(const GradRow& r, float scale, float x,
   const float z = scaled_difference(x, r.max, scale);
   float bonus = 0.0f;
   if (kEntropy) bonus = r.fb * (fmaxf(z - r.log_sum, kGone) + r.entropy);
-  if (is_target)  // a (1 - p), without the loss of 1 - p near 1
+  // a (1 - p) without a difference: near p = 1 as exact as log_sum, whose sum holds the
+  // largest logit's own 1, and so to 2^-24 of each addition, absolute
+  if (is_target)
     return (r.fa * expm1f(z - r.log_sum) + bonus * p) * r.unit;
   return (r.fa + bonus) * p * r.unit;
 }
