@@ -293,7 +293,10 @@ typedef struct tlc_train tlc_train;
  * max_dim values, and for lists of up to max_tensors tensors (at most
  * TLC_MAX_TENSORS).  Any of them may be 0: that call is then refused
  * (tlc_embedding needs none of them).  Allocates one device workspace of about
- * 1.1 MB + (24 + max_dim / 8) * max_tokens + max_rows bytes. */
+ * 1.1 MB + (24 + max_dim / 8) * max_tokens + max_rows bytes and, for more than 64
+ * tensors, which do not all travel with a launch's arguments, 24 * (4096 +
+ * max_tensors) bytes of it and 512 * (4096 + max_tensors) of pinned host memory
+ * (eight places for the pieces of a list: 2.1 MB for 65 tensors, 36 for 65536). */
 int tlc_train_create(tlc_train** ctx, size_t max_tokens, size_t max_rows, size_t max_dim,
                      size_t max_tensors, void* hip_stream);
 
