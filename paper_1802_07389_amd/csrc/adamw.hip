@@ -399,6 +399,8 @@ __global__ __launch_bounds__(kAdamThreads) void tlc_adamw_kernel(List list, Adam
     const int64_t step = a.clock->step + 1;
     shared = factors_of(a, step);
     if (a.result && blockIdx.x == 0) put_result(a.result, clip_of(a.result->sumsq, a.max_norm));
+    // (counted before the factors are released, which wait for it; it needs the clock's
+    // read alone)
     if (a.tickets && last_to_read(a.tickets, step) && !shared.skip) a.clock->step = step;
   }
   Step<kBits> s{a, &shared, {}};

@@ -246,7 +246,10 @@ struct TokenArgs : LogitArgs {
 // values 12.7 us, in blocks 17; with five alternatives 17.7 | 48.6), longer ones where
 // there are many or no alternatives are asked for (packs up to kManyPacks: 4096 rows
 // of 8192 bf16 values with twenty 22.9 | 34.5, 64 such rows 11.1 | 7.5).  More than
-// kWaveTop alternatives are half of a wave's lanes, whose largest then say little.
+// kWaveTop alternatives are half of a wave's lanes, whose largest then say little of long
+// segments: their rows take a block each.  That costs short rows much (4096 rows of 4096
+// bf16 values with 32 | 33 alternatives 16 | 48 us, 16384 of 64 values 24 | 150): of rows
+// of 64 packs and fewer, whose columns all fit in `found`, a wave has not been measured.
 constexpr uint32_t kWavePacks = 512, kManyPacks = 1024, kManyRows = 2048, kWaveTop = 32;
 inline bool wave_rows(uint32_t count, uint32_t packs, uint32_t top) {
   return top <= kWaveTop &&
