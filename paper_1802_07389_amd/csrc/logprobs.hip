@@ -507,8 +507,9 @@ __device__ __forceinline__ GradRow grad_row(const TokenGradArgs& a, uint32_t row
   r.live = r.target != kLeftOut && res.max != -INFINITY;
   if (!r.live) return GradRow{-1, 0.0f, 0.0f, 1.0f, 0.0f, 0.0f, 0.0f, false};  // 0 at x = 0
   // factors near fp32's end and beyond it are held as multiples of 2^80, as what p
-  // leaves of them may be small
-  const bool large = fmaxf(fabsf(ga), fabsf(gb)) * a.scale > 0x1p100f;
+  // leaves of them may be small (infinite ones are not: theirs is infinite)
+  const float most = fmaxf(fabsf(ga), fabsf(gb));
+  const bool large = most <= FLT_MAX && most * a.scale > 0x1p100f;
   const float s = large ? a.scale * 0x1p-80f : a.scale;
   r.unit = large ? 0x1p80f : 1.0f;
   r.fa = -(ga * s);

@@ -116,6 +116,23 @@ def test_factors_whose_product_with_the_scale_is_beyond_fp32(ctx, kind, scale, s
             assert not bool(got.isnan().any())
 
 
+@pytest.mark.parametrize("scale", [1e-30, 1.0, 1e18])
+def test_infinite_factors(ctx, scale):
+    """An infinite gradient is one at every p > 0, however small the scale."""
+    x = torch.zeros(4, 100, device="cuda")
+    t = torch.tensor([3, 50, 99, 0], device="cuda")
+    a = torch.tensor([math.inf, -math.inf, 2.0, math.inf], device="cuda")
+    r = ctx.token_logprobs(x, t, scale=scale)
+    got = ctx.token_logprobs_grad(x, t, r, a, None, scale=scale)
+    with_bonus = ctx.token_logprobs_grad(x, t, r, a, torch.ones_like(a), scale=scale)
+    ctx.sync()
+    want = torch.full_like(x, -math.inf)
+    want[1] = math.inf
+    want[torch.arange(4), t] = a
+    for d in (got, with_bonus):
+        assert torch.equal(d[[0, 1, 3]], want[[0, 1, 3]]) and bool(d[2].isfinite().all())
+
+
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 @pytest.mark.parametrize("scale,factor", [(0.5, 1.0), (3e-38, 1e20)])
 @pytest.mark.parametrize("masked", [False, True])
